@@ -417,6 +417,79 @@ int swaa_decode_num_blocks(int B, int Hq, int Hkv, int D, int Lmax, int window, 
 long long swaa_trimmed_cache_slot(long long pos, int window, int n_sink);
 long long swaa_trimmed_cache_len(long long len, int window, int n_sink);
 
+/*
+ * Queries, keys and values on their way from a projection to the attention: a norm of every query and key head and the rotation
+ * by the token's position, in one pass over the projection's output.  (The paper adapts models whose attention has both; it
+ * says nothing of them.)  For every head, with x its D channels:
+ *     y = weight * x / sqrt(mean(x^2) + eps)                                (without a weight: y = x)
+ *     (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position * inv_freq[i]
+ * for the pairs i = 0 .. rotary_dim/2 - 1 of the first rotary_dim channels: (a, b) = (i, i + rotary_dim/2), or (2i, 2i + 1) with
+ * interleaved != 0; channels from rotary_dim on keep y.  Values are copied.
+ *
+ *   q, k, v         device, bf16, [T, heads, D] with heads and channels dense and q_stride, k_stride, v_stride elements between
+ *                   tokens (>= heads * D, multiples of 8): the slices of one projection's output need no copy.  v and v_out may
+ *                   both be NULL.
+ *   q_weight, k_weight  device, float32 [D]; NULL: no norm of queries / keys.
+ *   eps             >= 0, added to the mean of the squares (fp32 sums).
+ *   inv_freq        device, float32 [rotary_dim / 2]; not needed with rotary_dim == 0 (no rotation).
+ *   rotary_dim      a multiple of 16, at most D.
+ *   positions       device, int32 [T], any value.  Angles are formed in double precision, so far positions lose nothing.
+ *   q_out, k_out, v_out  device, bf16, dense [T, Hq, D], [T, Hkv, D]: what swaa_prefill takes.  An output may be its own input
+ *                   (same address, dense); other overlaps are not allowed.
+ */
+int swaa_qk_norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                      const float* q_weight, const float* k_weight, float eps, const float* inv_freq, int rotary_dim,
+                      int interleaved, const int32_t* positions, int T, int Hq, int Hkv, int D, void* q_out, void* k_out,
+                      void* v_out, void* stream);
+
+/*
+ * Gradient of swaa_qk_norm_rope (Sec. 3.2.2: fine-tuning): from the gradients dq_out, dk_out (and dv_out) of its outputs, dense, and its
+ * inputs q, k, those of its inputs (dq, dk, dv, with strides between tokens like q, k, v) and of the weights (float32 [D],
+ * overwritten; sums over tokens and heads in a fixed order, so that a call repeats bit for bit on the same kind of GPU).  q (k) is
+ * not read, and may be NULL, without q_weight (k_weight); dq_weight (dk_weight) is NULL exactly when q_weight (k_weight) is; dv_out
+ * and dv may both be NULL.  dq, dk, dv may be the incoming gradients themselves (same address, dense) or the inputs q, k
+ * themselves (same address and stride).
+ *   workspace       device, at least swaa_qk_norm_rope_backward_workspace_size(T, Hq, Hkv, D) bytes, 256-byte aligned, uninitialised; not
+ *                   needed without weights.  Calls that may overlap need one each.
+ */
+size_t swaa_qk_norm_rope_backward_workspace_size(int T, int Hq, int Hkv, int D);
+int swaa_qk_norm_rope_backward(const void* q, const void* k, long long q_stride, long long k_stride, const void* dq_out,
+                               const void* dk_out, const void* dv_out, const float* q_weight, const float* k_weight, float eps,
+                               const float* inv_freq, int rotary_dim, int interleaved, const int32_t* positions, int T, int Hq,
+                               int Hkv, int D, void* dq, void* dk, void* dv, long long dq_stride, long long dk_stride,
+                               long long dv_stride, float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                               void* stream);
+
+/*
+ * The same pass at serving time: queries leave dense, keys and values go to their rows of the cache that swaa_decode,
+ * swaa_decode_paged or swaa_prefill_paged read next.  The batch is described as there: the new tokens of sequence b are
+ * cu_seqlens_q[b] .. cu_seqlens_q[b+1]-1 of the packed tokens and the last ones of its seqlens_k[b] entries, so that new token i is entry
+ * seqlens_k[b] - len_q + i of its sequence.
+ *   positions       device, int32 [Tq], of the rotation; NULL: the entry's index.  (After an eviction a sequence has fewer entries than
+ *                   positions.)
+ *   kcache, vcache  device, bf16 [B, Lmax, Hkv, D]; rows of other entries are left as they are.
+ *   window          0: entry j is row j, seqlens_k[b] <= Lmax.  > 0: the ring cache of a pure-SWA layer, row
+ *                   swaa_trimmed_cache_slot(j, window, n_sink), with n_sink + window <= Lmax and seqlens_k the number of tokens so far; of
+ *                   new tokens that meet in one row the last is stored.
+ *   kpages, vpages, block_table  as for swaa_prefill_paged (page_size a multiple of 64 here).  No two entries that a call writes
+ *                   may share a row.
+ *   q_out           device, bf16, dense [Tq, Hq, D].
+ * Tokens behind cu_seqlens_q[B] are padding: their rows of q_out are left as they are.  A sequence with more new tokens
+ * than entries, or more entries than the cache holds, is reported as SWAA_ERR_BAD_SEQLENS through the status word and nothing of
+ * it is written; a page index outside [0, num_pages) likewise, and the keys and values that would go there are not written.
+ * Other arguments as for swaa_qk_norm_rope.
+ */
+int swaa_cache_append(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                      const float* q_weight, const float* k_weight, float eps, const float* inv_freq, int rotary_dim,
+                      int interleaved, const int32_t* positions, const int32_t* cu_seqlens_q, const int32_t* seqlens_k, int B,
+                      int Tq, int Lmax, int Hq, int Hkv, int D, int window, int n_sink, void* q_out, void* kcache, void* vcache,
+                      void* stream);
+int swaa_cache_append_paged(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                            const float* q_weight, const float* k_weight, float eps, const float* inv_freq, int rotary_dim,
+                            int interleaved, const int32_t* positions, const int32_t* cu_seqlens_q, const int32_t* seqlens_k,
+                            const int32_t* block_table, int B, int Tq, int max_blocks, int num_pages, int page_size, int Hq,
+                            int Hkv, int D, void* q_out, void* kpages, void* vpages, void* stream);
+
 /* Static string for a swaa_status value. */
 const char* swaa_status_str(int status);
 /*

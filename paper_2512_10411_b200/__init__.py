@@ -22,6 +22,9 @@ from .binding import (  # noqa: F401
     schedule_is_full,
     schedule_select_fa_layers,
     status_str,
+    qk_norm_rope_backward_workspace_size,
+    swaa_cache_append,
+    swaa_cache_append_paged,
     swaa_decode,
     swaa_decode_paged,
     swaa_decode_partial,
@@ -31,6 +34,8 @@ from .binding import (  # noqa: F401
     swaa_decode_static,
     DECODE_STATIC_SCRATCH_BYTES,
     swaa_lazy_ratio,
+    swaa_qk_norm_rope,
+    swaa_qk_norm_rope_backward,
     swaa_prefill,
     swaa_prefill_backward,
     prefill_backward_workspace_size,

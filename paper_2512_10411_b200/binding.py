@@ -133,6 +133,18 @@ def load_library():
     lib.swaa_trimmed_cache_slot.restype = ctypes.c_longlong
     lib.swaa_trimmed_cache_len.argtypes = [ctypes.c_longlong, ci, ci]
     lib.swaa_trimmed_cache_len.restype = ctypes.c_longlong
+    ll, sz = ctypes.c_longlong, ctypes.c_size_t
+    lib.swaa_qk_norm_rope.argtypes = [vp] * 3 + [ll] * 3 + [vp, vp, cf, vp, ci, ci, vp, ci, ci, ci, ci] + [vp] * 4
+    lib.swaa_qk_norm_rope.restype = ci
+    lib.swaa_qk_norm_rope_backward_workspace_size.argtypes = [ci] * 4
+    lib.swaa_qk_norm_rope_backward_workspace_size.restype = sz
+    lib.swaa_qk_norm_rope_backward.argtypes = ([vp, vp, ll, ll] + [vp] * 5 + [cf, vp, ci, ci, vp, ci, ci, ci, ci] + [vp] * 3 + [ll] * 3 +
+                                               [vp, vp, vp, sz, vp])
+    lib.swaa_qk_norm_rope_backward.restype = ci
+    lib.swaa_cache_append.argtypes = [vp] * 3 + [ll] * 3 + [vp, vp, cf, vp, ci, ci] + [vp] * 3 + [ci] * 8 + [vp] * 4
+    lib.swaa_cache_append.restype = ci
+    lib.swaa_cache_append_paged.argtypes = [vp] * 3 + [ll] * 3 + [vp, vp, cf, vp, ci, ci] + [vp] * 4 + [ci] * 8 + [vp] * 4
+    lib.swaa_cache_append_paged.restype = ci
     lib.swaa_status_str.argtypes = [ci]
     lib.swaa_status_str.restype = ctypes.c_char_p
     lib.swaa_last_device_status.argtypes = [vp]
@@ -570,6 +582,152 @@ def swaa_decode_static(q, kcache, vcache, out, seqlens, window: int, n_sink: int
                                 D, int(window), int(n_sink), int(bool(is_full)), float(scale), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, "swaa_decode_static")
+
+
+def _on_current_device(t, where: str):
+    """Launches go to the current device: a tensor of another one is refused."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors must be on the current device")
+
+
+def _token_rows(t, H: int, D: int, name: str):
+    """(address, elements between tokens) of a bf16 tensor [T, H, D] whose heads and channels are dense."""
+    if t is None:
+        return None, H * D
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+        raise ValueError(f"{name}: heads and channels must be dense")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else H * D
+
+
+def _shaped(t, shape, where: str, name: str):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{where}: {name} must be {list(shape)}")
+
+
+def _rope_args(where, q, k, v, q_weight, k_weight, inv_freq):
+    """Sizes of the rotation's arguments, checked: (T, Hq, Hkv, D, rotary_dim)."""
+    _on_current_device(q, where)
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    _shaped(k, (T, Hkv, D), where, "k")
+    _shaped(v, (T, Hkv, D), where, "v")
+    _shaped(q_weight, (D,), where, "q_weight")
+    _shaped(k_weight, (D,), where, "k_weight")
+    if inv_freq is not None and inv_freq.dim() != 1:
+        raise ValueError(f"{where}: inv_freq must be [rotary_dim / 2]")
+    return T, Hq, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.numel()
+
+
+def swaa_qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k_out, v_out, eps: float = 1e-6, interleaved: bool = False,
+                      stream=None) -> None:
+    """Forwards to C swaa_qk_norm_rope.  q [T,Hq,D], k, v [T,Hkv,D] bf16, each with a stride of its own between tokens (slices of one
+    projection's output); q_weight, k_weight f32 [D] or None (no norm); inv_freq f32 [rotary_dim / 2] or None (no rotation); positions
+    int32 [T]; q_out [T,Hq,D], k_out, v_out [T,Hkv,D] bf16, contiguous.  v and v_out may both be None."""
+    lib = load_library()
+    where = "swaa_qk_norm_rope"
+    T, Hq, Hkv, D, rot = _rope_args(where, q, k, v, q_weight, k_weight, inv_freq)
+    _shaped(positions, (T,), where, "positions")
+    _shaped(q_out, (T, Hq, D), where, "q_out")
+    _shaped(k_out, (T, Hkv, D), where, "k_out")
+    _shaped(v_out, (T, Hkv, D), where, "v_out")
+    bf, f32 = torch.bfloat16, torch.float32
+    (qp, qs), (kp, ks), (vp, vs) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k"), _token_rows(v, Hkv, D, "v")
+    rc = lib.swaa_qk_norm_rope(qp, kp, vp, qs, ks, vs, _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
+                               _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)), _dev_ptr(positions, torch.int32, "positions"), T,
+                               Hq, Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(k_out, bf, "k_out"), _dev_ptr(v_out, bf, "v_out"),
+                               _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def qk_norm_rope_backward_workspace_size(T, Hq, Hkv, D) -> int:
+    """Forwards to C swaa_qk_norm_rope_backward_workspace_size (bytes)."""
+    return int(load_library().swaa_qk_norm_rope_backward_workspace_size(int(T), int(Hq), int(Hkv), int(D)))
+
+
+def swaa_qk_norm_rope_backward(q, k, dq_out, dk_out, dv_out, q_weight, k_weight, inv_freq, positions, dq, dk, dv, dq_weight, dk_weight,
+                               workspace, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """Forwards to C swaa_qk_norm_rope_backward.  q, k: the inputs of swaa_qk_norm_rope (None where they have no weight); dq_out, dk_out,
+    dv_out: gradients of its outputs, contiguous; dq, dk, dv: those of its inputs, each with a stride of its own between tokens;
+    dq_weight, dk_weight f32 [D] (None without the weight); workspace uint8 of qk_norm_rope_backward_workspace_size(T, Hq, Hkv, D) bytes
+    (None without weights).  dv_out and dv may both be None."""
+    lib = load_library()
+    where = "swaa_qk_norm_rope_backward"
+    T, Hq, Hkv, D, rot = _rope_args(where, dq_out, dk_out, dv_out, q_weight, k_weight, inv_freq)
+    for name, t, shp in (("q", q, (T, Hq, D)), ("k", k, (T, Hkv, D)), ("dq", dq, (T, Hq, D)), ("dk", dk, (T, Hkv, D)), ("dv", dv, (T, Hkv, D)),
+                         ("dq_weight", dq_weight, (D,)), ("dk_weight", dk_weight, (D,)), ("positions", positions, (T,))):
+        _shaped(t, shp, where, name)
+    bf, f32 = torch.bfloat16, torch.float32
+    (qp, qs), (kp, ks) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k")
+    (dqp, dqs), (dkp, dks), (dvp, dvs) = _token_rows(dq, Hq, D, "dq"), _token_rows(dk, Hkv, D, "dk"), _token_rows(dv, Hkv, D, "dv")
+    rc = lib.swaa_qk_norm_rope_backward(qp, kp, qs, ks, _dev_ptr(dq_out, bf, "dq_out"), _dev_ptr(dk_out, bf, "dk_out"), _dev_ptr(dv_out, bf, "dv_out"),
+                                        _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
+                                        _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)),
+                                        _dev_ptr(positions, torch.int32, "positions"), T, Hq, Hkv, D, dqp, dkp, dvp, dqs, dks, dvs,
+                                        _dev_ptr(dq_weight, f32, "dq_weight"), _dev_ptr(dk_weight, f32, "dk_weight"),
+                                        _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
+                                        _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved):
+    """The arguments that swaa_cache_append and swaa_cache_append_paged pass on first, and their sizes."""
+    T, Hq, Hkv, D, rot = _rope_args(where, q, k, v, q_weight, k_weight, inv_freq)
+    if v is None:
+        raise ValueError(f"{where}: v is needed")
+    B = cu_seqlens_q.numel() - 1
+    if seqlens_k.numel() != B:
+        raise ValueError(f"{where}: cu_seqlens_q must be [B + 1] and seqlens_k [B]")
+    _shaped(q_out, (T, Hq, D), where, "q_out")
+    _shaped(positions, (T,), where, "positions")
+    f32, i32 = torch.float32, torch.int32
+    (qp, qs), (kp, ks), (vp, vs) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k"), _token_rows(v, Hkv, D, "v")
+    return (qp, kp, vp, qs, ks, vs, _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
+            _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)), _dev_ptr(positions, i32, "positions"),
+            _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k")), B, T, Hq, Hkv, D
+
+
+def swaa_cache_append(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, kcache, vcache, positions=None, window: int = 0,
+                      n_sink: int = 0, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """Forwards to C swaa_cache_append.  q [Tq,Hq,D], k, v [Tq,Hkv,D] bf16 as in swaa_qk_norm_rope, packed by cu_seqlens_q int32 [B+1];
+    seqlens_k int32 [B]: entries of each sequence including the new ones; q_out [Tq,Hq,D] bf16; kcache, vcache [B,Lmax,Hkv,D] bf16;
+    positions int32 [Tq] or None (the entry's index); window > 0: the caches are rings as in trimmed_cache_slot."""
+    lib = load_library()
+    where = "swaa_cache_append"
+    args, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved)
+    Lmax = kcache.shape[1]
+    _shaped(kcache, (B, Lmax, Hkv, D), where, "kcache")
+    _shaped(vcache, (B, Lmax, Hkv, D), where, "vcache")
+    bf = torch.bfloat16
+    rc = lib.swaa_cache_append(*args, B, T, Lmax, Hq, Hkv, D, int(window), int(n_sink), _dev_ptr(q_out, bf, "q_out"),
+                               _dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, block_table, q_out, kpages, vpages, positions=None,
+                            eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """Forwards to C swaa_cache_append_paged: swaa_cache_append into kpages, vpages [num_pages,page_size,Hkv,D] bf16 through
+    block_table int32 [B,max_blocks]."""
+    lib = load_library()
+    where = "swaa_cache_append_paged"
+    args, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved)
+    num_pages, page_size = kpages.shape[:2]
+    _shaped(kpages, (num_pages, page_size, Hkv, D), where, "kpages")
+    _shaped(vpages, (num_pages, page_size, Hkv, D), where, "vpages")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"{where}: block_table must be [B, max_blocks]")
+    bf = torch.bfloat16
+    rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, block_table.shape[1], num_pages, page_size, Hq,
+                                     Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"),
+                                     _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
 
 
 def schedule_is_full(policy: SwaaPolicy, layer: int, phase: int) -> bool:

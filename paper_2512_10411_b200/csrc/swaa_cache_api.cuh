@@ -1,0 +1,225 @@
+// C-ABI entry points of the operators around the key/value cache: validation, planning and launches (see include/swaa.h).
+// Part of the translation unit of swaa_lib.cu, which includes it last.
+#pragma once
+
+#include "swaa_rope.cuh"
+
+namespace swaa {
+
+static bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+static bool stride_ok(long long stride, int heads, int D) { return stride % 8 == 0 && stride >= (long long)heads * D; }
+
+// What the packed form, the cache form and the gradient have in common.
+static int check_rope(int T, int Hq, int Hkv, int D, int rotary_dim, const float* inv_freq, const float* qw, const float* kw, float eps) {
+    if (T < 0 || Hq < 1 || Hkv < 1 || rotary_dim < 0 || !(eps >= 0.f)) return SWAA_ERR_INVALID_ARG;
+    if (Hq % Hkv != 0 || (D != 64 && D != 128)) return SWAA_ERR_UNSUPPORTED;
+    if (rotary_dim > D || rotary_dim % 16 != 0) return SWAA_ERR_UNSUPPORTED;
+    if ((rotary_dim > 0 && !inv_freq) || !aligned4(inv_freq) || !aligned4(qw) || !aligned4(kw)) return SWAA_ERR_INVALID_ARG;
+    if (Hq > (1 << 20)) return SWAA_ERR_UNSUPPORTED;
+    return SWAA_OK;
+}
+
+// Warps' shares of one token: groups of heads of one kind.
+template <typename P>
+static void rope_segments(P* p, int Hq, int Hkv, int D, int rows, bool values) {
+    const int per = rows * (32 / (D / 16));
+    p->seg_q = (Hq + per - 1) / per;
+    p->seg_k = (Hkv + per - 1) / per;
+    p->segs = p->seg_q + p->seg_k * (values ? 2 : 1);
+}
+
+// Blocks of a launch: one warp per share of a token, as many as the SMs hold at a time; the warps go on through the tokens.
+static unsigned rope_blocks(int T, int segs, int sms, int per_sm) {
+    const long long most = std::max((long long)sms * per_sm, ((long long)segs + kRopeWarps - 1) / kRopeWarps);
+    return (unsigned)std::min(((long long)T * segs + kRopeWarps - 1) / kRopeWarps, most);
+}
+
+constexpr int kRopeBlocksPerSm = 3, kRopeBwdBlocksPerSm = 2;
+
+template <bool kCache>
+static int launch_rope(const RopeParams& p, int D, bool pairs, int sms, cudaStream_t st) {
+    const dim3 grid(rope_blocks(p.T, p.segs, sms, kRopeBlocksPerSm));
+    auto* kernel = D == 128 ? (pairs ? rope_kernel<128, true, kCache> : rope_kernel<128, false, kCache>)
+                            : (pairs ? rope_kernel<64, true, kCache> : rope_kernel<64, false, kCache>);
+    return launch_overlapped(kernel, grid, kRopeThreads, 0, st, p);
+}
+
+static int current_sm100(DeviceInfo* info) {
+    const int rc = current_device_info(info);
+    if (rc != SWAA_OK) return rc;
+    return info->cc_major == 10 ? SWAA_OK : SWAA_ERR_UNSUPPORTED;
+}
+
+static RopeParams rope_params(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                              const float* qw, const float* kw, float eps, const float* inv_freq, const int32_t* positions, int T, int Hq,
+                              int Hkv, int D, int rotary_dim, void* q_out, void* k_out, void* v_out) {
+    RopeParams p = {};
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.v = static_cast<const __nv_bfloat16*>(v);
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.v_stride = v_stride;
+    p.qw = qw;
+    p.kw = kw;
+    p.eps = eps;
+    p.inv_freq = inv_freq;
+    p.positions = positions;
+    p.T = T;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.rot = rotary_dim;
+    p.q_out = static_cast<__nv_bfloat16*>(q_out);
+    p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.v_out = static_cast<__nv_bfloat16*>(v_out);
+    rope_segments(&p, Hq, Hkv, D, kRopeRows, v != nullptr);
+    return p;
+}
+
+// Shared body of swaa_cache_append (block_table == nullptr) and swaa_cache_append_paged.
+static int append_impl(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                       const float* qw, const float* kw, float eps, const float* inv_freq, int rotary_dim, int interleaved,
+                       const int32_t* positions, const int32_t* cu_seqlens_q, const int32_t* seqlens_k, const int32_t* block_table, int B,
+                       int Tq, int rows, int max_blocks, int num_pages, int page_size, int Hq, int Hkv, int D, int window, int n_sink,
+                       void* q_out, void* kcache, void* vcache, void* stream) {
+    if (B < 0 || rows < 1 || window < 0 || n_sink < 0) return SWAA_ERR_INVALID_ARG;
+    int rc = check_rope(Tq, Hq, Hkv, D, rotary_dim, inv_freq, qw, kw, eps);
+    if (rc != SWAA_OK) return rc;
+    if (!stride_ok(q_stride, Hq, D) || !stride_ok(k_stride, Hkv, D) || !stride_ok(v_stride, Hkv, D)) return SWAA_ERR_INVALID_ARG;
+    if (window > 0 && (long long)n_sink + window > rows) return SWAA_ERR_INVALID_ARG;  // the ring does not fit the cache
+    if (B == 0 || Tq == 0) return SWAA_OK;
+    if (!q || !k || !v || !cu_seqlens_q || !seqlens_k || !q_out || !kcache || !vcache) return SWAA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(kcache) || !aligned16(vcache)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned4(positions) || !aligned4(cu_seqlens_q) || !aligned4(seqlens_k) || !aligned4(block_table)) return SWAA_ERR_INVALID_ARG;
+    DeviceInfo info;
+    if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
+    RopeParams p = rope_params(q, k, v, q_stride, k_stride, v_stride, qw, kw, eps, inv_freq, positions, Tq, Hq, Hkv, D, rotary_dim, q_out,
+                               kcache, vcache);
+    p.cu = cu_seqlens_q;
+    p.seqlens = seqlens_k;
+    p.block_table = block_table;
+    p.B = B;
+    p.rows = rows;
+    p.max_blocks = max_blocks;
+    p.page_size = page_size;
+    p.num_pages = num_pages;
+    p.ring = window;
+    p.n_sink = n_sink;
+    return launch_rope<true>(p, D, interleaved != 0, info.sm_count, reinterpret_cast<cudaStream_t>(stream));
+}
+
+}  // namespace swaa
+
+// ----------------------------------------------------------------------------------- norm and rotation
+extern "C" int swaa_qk_norm_rope(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                                 const float* q_weight, const float* k_weight, float eps, const float* inv_freq, int rotary_dim,
+                                 int interleaved, const int32_t* positions, int T, int Hq, int Hkv, int D, void* q_out, void* k_out,
+                                 void* v_out, void* stream) {
+    int rc = check_rope(T, Hq, Hkv, D, rotary_dim, inv_freq, q_weight, k_weight, eps);
+    if (rc != SWAA_OK) return rc;
+    if (!stride_ok(q_stride, Hq, D) || !stride_ok(k_stride, Hkv, D) || (v && !stride_ok(v_stride, Hkv, D))) return SWAA_ERR_INVALID_ARG;
+    if (T == 0) return SWAA_OK;
+    if (!q || !k || !q_out || !k_out || !positions || (v == nullptr) != (v_out == nullptr)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out) || !aligned4(positions))
+        return SWAA_ERR_INVALID_ARG;
+    DeviceInfo info;
+    if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
+    const RopeParams p = rope_params(q, k, v, q_stride, k_stride, v_stride, q_weight, k_weight, eps, inv_freq, positions, T, Hq, Hkv, D,
+                                     rotary_dim, q_out, k_out, v_out);
+    return launch_rope<false>(p, D, interleaved != 0, info.sm_count, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t swaa_qk_norm_rope_backward_workspace_size(int T, int Hq, int Hkv, int D) {
+    if (T < 1 || check_rope(T, Hq, Hkv, D, 0, nullptr, nullptr, nullptr, 0.f) != SWAA_OK) return 256;
+    DeviceInfo info;
+    if (current_device_info(&info) != SWAA_OK) info.sm_count = 148;
+    RopeGradParams p;
+    rope_segments(&p, Hq, Hkv, D, kRopeBwdRows, true);  // values or not: the more blocks
+    return (size_t)rope_blocks(T, p.segs, info.sm_count, kRopeBwdBlocksPerSm) * 2 * D * sizeof(float);
+}
+
+extern "C" int swaa_qk_norm_rope_backward(const void* q, const void* k, long long q_stride, long long k_stride, const void* dq_out,
+                                          const void* dk_out, const void* dv_out, const float* q_weight, const float* k_weight, float eps,
+                                          const float* inv_freq, int rotary_dim, int interleaved, const int32_t* positions, int T, int Hq,
+                                          int Hkv, int D, void* dq, void* dk, void* dv, long long dq_stride, long long dk_stride,
+                                          long long dv_stride, float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                                          void* stream) {
+    int rc = check_rope(T, Hq, Hkv, D, rotary_dim, inv_freq, q_weight, k_weight, eps);
+    if (rc != SWAA_OK) return rc;
+    if ((q_weight && !stride_ok(q_stride, Hq, D)) || (k_weight && !stride_ok(k_stride, Hkv, D)) || !stride_ok(dq_stride, Hq, D) ||
+        !stride_ok(dk_stride, Hkv, D) || (dv && !stride_ok(dv_stride, Hkv, D)))
+        return SWAA_ERR_INVALID_ARG;
+    // a weight and its gradient come together
+    if ((q_weight == nullptr) != (dq_weight == nullptr) || (k_weight == nullptr) != (dk_weight == nullptr)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned4(dq_weight) || !aligned4(dk_weight)) return SWAA_ERR_INVALID_ARG;
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    if (T == 0) {  // sums over no tokens
+        if (dq_weight && cudaMemsetAsync(dq_weight, 0, D * sizeof(float), st) != cudaSuccess) return SWAA_ERR_CUDA;
+        if (dk_weight && cudaMemsetAsync(dk_weight, 0, D * sizeof(float), st) != cudaSuccess) return SWAA_ERR_CUDA;
+        return SWAA_OK;
+    }
+    if ((q_weight && !q) || (k_weight && !k) || !dq_out || !dk_out || !dq || !dk || !positions || (dv_out == nullptr) != (dv == nullptr))
+        return SWAA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dv_out) || !aligned16(dq) || !aligned16(dk) ||
+        !aligned16(dv) || !aligned4(positions))
+        return SWAA_ERR_INVALID_ARG;
+    DeviceInfo info;
+    if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
+    RopeGradParams p = {};
+    rope_segments(&p, Hq, Hkv, D, kRopeBwdRows, dv != nullptr);
+    const unsigned blocks = rope_blocks(T, p.segs, info.sm_count, kRopeBwdBlocksPerSm);
+    const bool weights = q_weight != nullptr || k_weight != nullptr;
+    if (weights && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < (size_t)blocks * 2 * D * sizeof(float)))
+        return SWAA_ERR_WORKSPACE;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.q_stride = q_stride;
+    p.k_stride = k_stride;
+    p.dq_out = static_cast<const __nv_bfloat16*>(dq_out);
+    p.dk_out = static_cast<const __nv_bfloat16*>(dk_out);
+    p.dv_out = static_cast<const __nv_bfloat16*>(dv_out);
+    p.qw = q_weight;
+    p.kw = k_weight;
+    p.eps = eps;
+    p.inv_freq = inv_freq;
+    p.positions = positions;
+    p.T = T;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.rot = rotary_dim;
+    p.dq = static_cast<__nv_bfloat16*>(dq);
+    p.dk = static_cast<__nv_bfloat16*>(dk);
+    p.dv = static_cast<__nv_bfloat16*>(dv);
+    p.dq_stride = dq_stride;
+    p.dk_stride = dk_stride;
+    p.dv_stride = dv_stride;
+    p.partial = weights ? static_cast<float*>(workspace) : nullptr;
+    auto* kernel = D == 128 ? (interleaved ? rope_backward_kernel<128, true> : rope_backward_kernel<128, false>)
+                            : (interleaved ? rope_backward_kernel<64, true> : rope_backward_kernel<64, false>);
+    rc = launch_overlapped(kernel, dim3(blocks), kRopeThreads, 0, st, p);
+    if (rc != SWAA_OK || !weights) return rc;
+    return launch_overlapped(rope_weight_grad_kernel, dim3((unsigned)(2 * D / 32)), 1024, 0, st, p.partial, (int)blocks, D, dq_weight, dk_weight);
+}
+
+// -------------------------------------------------------------------------------------- cache append
+extern "C" int swaa_cache_append(const void* q, const void* k, const void* v, long long q_stride, long long k_stride, long long v_stride,
+                                 const float* q_weight, const float* k_weight, float eps, const float* inv_freq, int rotary_dim,
+                                 int interleaved, const int32_t* positions, const int32_t* cu_seqlens_q, const int32_t* seqlens_k, int B,
+                                 int Tq, int Lmax, int Hq, int Hkv, int D, int window, int n_sink, void* q_out, void* kcache, void* vcache,
+                                 void* stream) {
+    return append_impl(q, k, v, q_stride, k_stride, v_stride, q_weight, k_weight, eps, inv_freq, rotary_dim, interleaved, positions,
+                       cu_seqlens_q, seqlens_k, nullptr, B, Tq, Lmax, 0, 0, 0, Hq, Hkv, D, window, n_sink, q_out, kcache, vcache, stream);
+}
+
+extern "C" int swaa_cache_append_paged(const void* q, const void* k, const void* v, long long q_stride, long long k_stride,
+                                       long long v_stride, const float* q_weight, const float* k_weight, float eps, const float* inv_freq,
+                                       int rotary_dim, int interleaved, const int32_t* positions, const int32_t* cu_seqlens_q,
+                                       const int32_t* seqlens_k, const int32_t* block_table, int B, int Tq, int max_blocks, int num_pages,
+                                       int page_size, int Hq, int Hkv, int D, void* q_out, void* kpages, void* vpages, void* stream) {
+    const int rc = check_paged_shape(max_blocks, num_pages, page_size);
+    if (rc != SWAA_OK) return rc;
+    if (!block_table) return SWAA_ERR_INVALID_ARG;
+    return append_impl(q, k, v, q_stride, k_stride, v_stride, q_weight, k_weight, eps, inv_freq, rotary_dim, interleaved, positions,
+                       cu_seqlens_q, seqlens_k, block_table, B, Tq, max_blocks * page_size, max_blocks, num_pages, page_size, Hq, Hkv, D, 0,
+                       0, q_out, kpages, vpages, stream);
+}

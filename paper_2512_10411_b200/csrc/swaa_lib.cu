@@ -1193,3 +1193,6 @@ extern "C" int swaa_last_device_status(void* stream) {
 }
 
 extern "C" uint64_t swaa_kernel_launch_count(void) { return launch_counter().load(std::memory_order_relaxed); }
+
+// The operators around the key/value cache.
+#include "swaa_cache_api.cuh"

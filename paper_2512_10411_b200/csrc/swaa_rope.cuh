@@ -1,0 +1,407 @@
+// Queries, keys and values on their way from the projection to the attention: a norm of every query and key head, the
+// rotation by the token's position, and the store into what the attention reads (packed rows, or the rows of a
+// dense, ring or paged key/value cache), in one pass; and the gradient of the packed form.
+//
+//     u = x / sqrt(mean(x^2) + eps)          over the D channels of one head of one token
+//     y = w u                                 (w: one weight per channel; without weights y = x)
+//     (z_a, z_b) = (y_a cos - y_b sin, y_b cos + y_a sin)      for every pair (a, b) of the first R channels
+// with the angle position * frequency of the pair; pairs are (i, i + R/2), or (2i, 2i + 1) when interleaved.  The channels from R on
+// keep y.  Gradient, with g = the rotation by the negative angle of dz:
+//     dw = sum over tokens and heads of g u,     dx = (w g - u mean(w g u)) / sqrt(mean(x^2) + eps)
+//
+// Angles are formed in double: position * frequency / 2 pi keeps its fraction to 2^-24 for every 32-bit position, and
+// sincospif takes the fraction; there is no table whose length bounds the positions.  All sums and products are
+// fp32, rounded to bf16 once, at the store.
+//
+// What bounds it: memory, every channel read and written once (2 * 2 bytes a channel; the gradient 3 * 2).  A head is D / 16 lanes,
+// each with two 16-byte pieces that hold both channels of its pairs, so the rotation needs no exchange and the norm log2(D / 16)
+// shuffles.  A warp takes kRopeRows groups of 32 / (D / 16) heads of one kind (query, key, value) of one token, all
+// its loads in flight at once; the frequencies of a token are spread over the lanes that hold the same channels of different heads,
+// so that a lane forms 8 / (heads per group) of its 8 angles and takes the others by shuffle.
+#pragma once
+
+#include "swaa_internal.cuh"
+#include "swaa_ptx.cuh"
+
+namespace swaa {
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeRows = 4;     // groups of heads that a warp has in flight: forward
+constexpr int kRopeBwdRows = 2;  // and gradient, which holds two rows of each
+
+struct RopeParams {
+    const __nv_bfloat16 *q, *k, *v;              // [T, heads, D] with a stride between tokens
+    long long q_stride, k_stride, v_stride;      // elements
+    const float *qw, *kw;                        // [D] or null
+    float eps;
+    const float* inv_freq;                       // [rot / 2]
+    const int32_t* positions;                    // [T]; cache form: may be null
+    int T, Hq, Hkv, rot;
+    int seg_q, seg_k, segs;                      // warps' shares of a token's query heads, key heads, all
+    __nv_bfloat16 *q_out, *k_out, *v_out;        // packed [T, heads, D]; cache form: k_out, v_out are the cache
+    // cache form
+    const int32_t *cu, *seqlens, *block_table;   // block_table null: dense [B, rows, Hkv, D]
+    int B, rows /* of a sequence: Lmax, or max_blocks * page_size */, max_blocks, page_size, num_pages;
+    int ring, n_sink;                            // ring > 0: slots n_sink .. n_sink + ring - 1 are a ring
+};
+
+struct RopeGradParams {
+    const __nv_bfloat16 *q, *k;                  // inputs of the forward pass (null where not normalised)
+    long long q_stride, k_stride;
+    const __nv_bfloat16 *dq_out, *dk_out, *dv_out;  // packed
+    const float *qw, *kw;
+    float eps;
+    const float* inv_freq;
+    const int32_t* positions;
+    int T, Hq, Hkv, rot;
+    int seg_q, seg_k, segs;
+    __nv_bfloat16 *dq, *dk, *dv;
+    long long dq_stride, dk_stride, dv_stride;
+    float* partial;                              // [blocks][2][D]: weight gradients of a block
+};
+
+// What a lane holds of a head: 8 channels from a0 and 8 from b0; pair i is (a_i, b_i), or, interleaved, pairs 0..3 are the
+// neighbours in a and 4..7 those in b.  rot_a, rot_b: whether the pieces are rotated.
+template <int D, bool kPairs>
+struct RopeLane {
+    static constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kAngles = 8 / kHeads;
+    int l, sub, a0, b0;
+    bool rot_a, rot_b;
+    float f[kAngles];
+    __device__ __forceinline__ RopeLane(int lane, const float* inv_freq, int rot) {
+        l = lane % kLanes;
+        sub = lane / kLanes;
+        const int np = rot / 16;  // half-split: lanes whose pieces are the two halves of pairs
+        if (kPairs) {
+            a0 = 8 * l;
+            b0 = 8 * (l + kLanes);
+            rot_a = a0 < rot;
+            rot_b = b0 < rot;
+        } else {
+            a0 = l < np ? 8 * l : 16 * np + 16 * (l - np);
+            b0 = l < np ? 8 * (l + np) : a0 + 8;
+            rot_a = rot_b = l < np;
+        }
+#pragma unroll
+        for (int i = 0; i < kAngles; ++i) {
+            const int pair = sub * kAngles + i;  // of the lane's 8
+            const bool turned = kPairs ? (pair < 4 ? rot_a : rot_b) : rot_a;
+            const int at = kPairs ? (pair < 4 ? a0 / 2 + pair : b0 / 2 + pair - 4) : 8 * l + pair;
+            f[i] = turned ? inv_freq[at] : 0.f;
+        }
+    }
+    // cos and sin of the lane's 8 pairs at a position
+    __device__ __forceinline__ void turn(int position, float (&c)[8], float (&s)[8]) const {
+        float cm[kAngles], sm[kAngles];
+#pragma unroll
+        for (int i = 0; i < kAngles; ++i) {
+            const double t = (double)position * (double)f[i] * 0.15915494309189533577;  // 1 / (2 pi)
+            sincospif(2.f * (float)(t - rint(t)), &sm[i], &cm[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            c[i] = __shfl_sync(0xffffffffu, cm[i % kAngles], (i / kAngles) * kLanes + l);
+            s[i] = __shfl_sync(0xffffffffu, sm[i % kAngles], (i / kAngles) * kLanes + l);
+        }
+    }
+    // Rotation by the angle, or by its negative.  Pieces that are not rotated pass as they are (no 0 * inf).
+    template <bool kBack>
+    __device__ __forceinline__ void rotate(float (&a)[8], float (&b)[8], const float (&c)[8], const float (&s)[8]) const {
+        auto pair = [](float& x, float& y, float co, float si, bool on) {
+            const float sn = kBack ? -si : si;
+            const float x1 = x * co - y * sn, y1 = y * co + x * sn;
+            x = on ? x1 : x;
+            y = on ? y1 : y;
+        };
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (!kPairs) pair(a[i], b[i], c[i], s[i], rot_a);
+            else if (i < 4) pair(a[2 * i], a[2 * i + 1], c[i], s[i], rot_a);
+            else pair(b[2 * i - 8], b[2 * i - 7], c[i], s[i], rot_b);
+        }
+    }
+    static __device__ __forceinline__ float sum(float x) {  // over the lanes of a head
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return x;
+    }
+};
+
+__device__ __forceinline__ void unpack_bf16x8(const uint4& v, float (&x)[8]) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(u[i] << 16);
+        x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack_bf16x8(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+// 8 weights of a piece; ones where there are none
+__device__ __forceinline__ void load_weights(const float* w, int at, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = w != nullptr ? w[at + i] : 1.f;
+}
+
+// Sequence that owns packed token t: the smallest b with cu[b + 1] > t, or B behind the last one.  All lanes of the warp
+// look at 32 places at a time.  Whatever cu holds, every index stays in [0, B].
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int t, int lane) {
+    int lo = 0, n = B;
+    while (n > 0) {
+        const int step = (n + 31) / 32;
+        const long long ahead = (long long)(lane + 1) * step;
+        const int at = lo + (int)(ahead < n ? ahead : n);  // cu[at] ends a stretch of `step` sequences
+        const unsigned hit = __ballot_sync(0xffffffffu, cu[at] > t);
+        if (hit == 0u) return B;
+        const int first = (__ffs((int)hit) - 1) * step;
+        lo += first < n ? first : n - 1;
+        if (step == 1) return lo;
+        n = n - first < step ? n - first : step;
+    }
+    return B;
+}
+
+// Where a token of the cache form goes.
+struct RopeToken {
+    bool valid;     // belongs to a sequence whose lengths are consistent
+    int position;
+    long long row;  // of the cache seen as [rows, Hkv, D]; -1: keys and values are not stored
+};
+__device__ __forceinline__ RopeToken rope_token(const RopeParams& p, int t, int lane) {
+    RopeToken r = {false, 0, -1};
+    const int b = sequence_of(p.cu, p.B, t, lane);
+    if (b >= p.B) return r;  // behind the last sequence: padding, left alone
+    const int start = p.cu[b], end = p.cu[b + 1], len = p.seqlens[b];
+    // (a token is looked for only where cu says that it is; start > t or a length beyond the tokens shows a cu that decreases)
+    if (start < 0 || start > t || end > p.T || (long long)end - start > len || (p.ring == 0 && len > p.rows)) {
+        record_device_error(SWAA_ERR_BAD_SEQLENS);
+        return r;
+    }
+    const int e = len - (end - t);  // index of the token in its sequence
+    r.valid = true;
+    r.position = p.positions != nullptr ? p.positions[t] : e;
+    int slot = e;
+    if (p.ring > 0 && e >= p.n_sink) {
+        if ((long long)e + p.ring < len) return r;  // a later token of the call has the slot
+        slot = p.n_sink + (e - p.n_sink) % p.ring;
+    }
+    if (p.block_table == nullptr) {
+        r.row = (long long)b * p.rows + slot;
+    } else {
+        const int page = p.block_table[(size_t)b * p.max_blocks + slot / p.page_size];
+        if (page < 0 || page >= p.num_pages) record_device_error(SWAA_ERR_BAD_SEQLENS);
+        else r.row = (long long)page * p.page_size + slot % p.page_size;
+    }
+    return r;
+}
+
+template <int D, bool kPairs, bool kCache>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
+    using L = RopeLane<D, kPairs>;
+    grid_wait();
+    const int lane = threadIdx.x & 31;
+    const unsigned warp = blockIdx.x * kRopeWarps + (threadIdx.x >> 5), warps = gridDim.x * kRopeWarps;
+    const int seg = (int)(warp % (unsigned)p.segs), stream = (int)(warp / (unsigned)p.segs), streams = (int)(warps / (unsigned)p.segs);
+    if (stream >= streams) return;
+    const int kind = seg < p.seg_q ? 0 : seg < p.seg_q + p.seg_k ? 1 : 2;
+    const int heads = kind == 0 ? p.Hq : p.Hkv;
+    const int h0 = (seg - (kind == 0 ? 0 : kind == 1 ? p.seg_q : p.seg_q + p.seg_k)) * (L::kHeads * kRopeRows);
+    const __nv_bfloat16* in = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
+    const long long stride = kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride;
+    __nv_bfloat16* out = kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out;
+    const float* w = kind == 0 ? p.qw : kind == 1 ? p.kw : nullptr;
+    const L ln(lane, p.inv_freq, kind == 2 ? 0 : p.rot);
+    const bool norm = w != nullptr;
+    float wa[8], wb[8];
+    load_weights(w, ln.a0, wa);
+    load_weights(w, ln.b0, wb);
+    for (int t = stream; t < p.T; t += streams) {
+        uint4 xa[kRopeRows], xb[kRopeRows];
+#pragma unroll
+        for (int u = 0; u < kRopeRows; ++u) {
+            const int h = h0 + u * L::kHeads + ln.sub;
+            if (h < heads) {
+                const __nv_bfloat16* x = in + t * stride + (long long)h * D;
+                xa[u] = *reinterpret_cast<const uint4*>(x + ln.a0);
+                xb[u] = *reinterpret_cast<const uint4*>(x + ln.b0);
+            } else {
+                xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        int position = 0;
+        long long row = t;
+        if (kCache) {
+            const RopeToken at = rope_token(p, t, lane);  // the same for the whole warp
+            if (!at.valid) continue;
+            position = at.position;
+            if (kind != 0) row = at.row;
+            if (row < 0) continue;
+        } else if (kind != 2) {
+            position = p.positions[t];
+        }
+        float c[8], s[8];
+        if (kind != 2) ln.turn(position, c, s);
+#pragma unroll
+        for (int u = 0; u < kRopeRows; ++u) {
+            if (h0 + u * L::kHeads >= heads) break;  // uniform
+            const int h = h0 + u * L::kHeads + ln.sub;
+            if (kind != 2) {
+                float a[8], b[8];
+                unpack_bf16x8(xa[u], a);
+                unpack_bf16x8(xb[u], b);
+                if (norm) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
+                    const float r = rsqrtf(L::sum(ss) * (1.f / D) + p.eps);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        a[i] *= r * wa[i];
+                        b[i] *= r * wb[i];
+                    }
+                }
+                ln.template rotate<false>(a, b, c, s);
+                xa[u] = pack_bf16x8(a);
+                xb[u] = pack_bf16x8(b);
+            }
+            if (h < heads) {
+                __nv_bfloat16* y = out + (row * heads + h) * D;
+                *reinterpret_cast<uint4*>(y + ln.a0) = xa[u];
+                *reinterpret_cast<uint4*>(y + ln.b0) = xb[u];
+            }
+        }
+    }
+}
+
+template <int D, bool kPairs>
+__global__ void __launch_bounds__(kRopeThreads) rope_backward_kernel(const RopeGradParams p) {
+    using L = RopeLane<D, kPairs>;
+    __shared__ float sm_w[kRopeWarps][D];
+    grid_wait();
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const unsigned warp = blockIdx.x * kRopeWarps + wid, warps = gridDim.x * kRopeWarps;
+    const int seg = (int)(warp % (unsigned)p.segs), stream = (int)(warp / (unsigned)p.segs), streams = (int)(warps / (unsigned)p.segs);
+    const int kind = seg < p.seg_q ? 0 : seg < p.seg_q + p.seg_k ? 1 : 2;
+    const int heads = kind == 0 ? p.Hq : p.Hkv;
+    const int h0 = (seg - (kind == 0 ? 0 : kind == 1 ? p.seg_q : p.seg_q + p.seg_k)) * (L::kHeads * kRopeBwdRows);
+    const __nv_bfloat16* x_in = kind == 0 ? p.q : p.k;
+    const long long x_stride = kind == 0 ? p.q_stride : p.k_stride;
+    const __nv_bfloat16* dy_in = kind == 0 ? p.dq_out : kind == 1 ? p.dk_out : p.dv_out;
+    __nv_bfloat16* dx = kind == 0 ? p.dq : kind == 1 ? p.dk : p.dv;
+    const long long dx_stride = kind == 0 ? p.dq_stride : kind == 1 ? p.dk_stride : p.dv_stride;
+    const float* w = kind == 0 ? p.qw : kind == 1 ? p.kw : nullptr;
+    const L ln(lane, p.inv_freq, kind == 2 ? 0 : p.rot);
+    const bool norm = w != nullptr;
+    float wa[8], wb[8], da[8], db[8];
+    load_weights(w, ln.a0, wa);
+    load_weights(w, ln.b0, wb);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) da[i] = db[i] = 0.f;
+    for (int t = stream; t < p.T && stream < streams; t += streams) {
+        uint4 ya[kRopeBwdRows], yb[kRopeBwdRows], xa[kRopeBwdRows], xb[kRopeBwdRows];
+#pragma unroll
+        for (int u = 0; u < kRopeBwdRows; ++u) {
+            const int h = h0 + u * L::kHeads + ln.sub;
+            ya[u] = yb[u] = xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
+            if (h < heads) {
+                const __nv_bfloat16* y = dy_in + ((long long)t * heads + h) * D;
+                ya[u] = *reinterpret_cast<const uint4*>(y + ln.a0);
+                yb[u] = *reinterpret_cast<const uint4*>(y + ln.b0);
+                if (norm) {
+                    const __nv_bfloat16* x = x_in + t * x_stride + (long long)h * D;
+                    xa[u] = *reinterpret_cast<const uint4*>(x + ln.a0);
+                    xb[u] = *reinterpret_cast<const uint4*>(x + ln.b0);
+                }
+            }
+        }
+        float c[8], s[8];
+        if (kind != 2) ln.turn(p.positions[t], c, s);
+#pragma unroll
+        for (int u = 0; u < kRopeBwdRows; ++u) {
+            if (h0 + u * L::kHeads >= heads) break;  // uniform
+            const int h = h0 + u * L::kHeads + ln.sub;
+            if (kind != 2) {
+                float ga[8], gb[8];
+                unpack_bf16x8(ya[u], ga);
+                unpack_bf16x8(yb[u], gb);
+                ln.template rotate<true>(ga, gb, c, s);
+                if (norm) {
+                    float a[8], b[8], ss = 0.f;
+                    unpack_bf16x8(xa[u], a);
+                    unpack_bf16x8(xb[u], b);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
+                    const float r = rsqrtf(L::sum(ss) * (1.f / D) + p.eps);
+                    float dot = 0.f;  // sum of (w g) u
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        a[i] *= r;
+                        b[i] *= r;
+                        da[i] += ga[i] * a[i];  // rows past the last head hold zeros
+                        db[i] += gb[i] * b[i];
+                        ga[i] *= wa[i];
+                        gb[i] *= wb[i];
+                        dot += ga[i] * a[i] + gb[i] * b[i];
+                    }
+                    dot = L::sum(dot) * (1.f / D);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        ga[i] = r * (ga[i] - a[i] * dot);
+                        gb[i] = r * (gb[i] - b[i] * dot);
+                    }
+                }
+                ya[u] = pack_bf16x8(ga);
+                yb[u] = pack_bf16x8(gb);
+            }
+            if (h < heads) {
+                __nv_bfloat16* x = dx + t * dx_stride + (long long)h * D;
+                *reinterpret_cast<uint4*>(x + ln.a0) = ya[u];
+                *reinterpret_cast<uint4*>(x + ln.b0) = yb[u];
+            }
+        }
+    }
+    if (p.partial == nullptr) return;
+    // weight gradients: the lanes with the same channels, then the block's warps in order, then (the next kernel) the blocks in order
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int o = L::kLanes; o < 32; o <<= 1) {
+            da[i] += __shfl_xor_sync(0xffffffffu, da[i], o);
+            db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+        }
+        if (ln.sub == 0) {
+            sm_w[wid][ln.a0 + i] = da[i];
+            sm_w[wid][ln.b0 + i] = db[i];
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += kRopeThreads) {
+        float sum = 0.f;
+        for (int o = 0; o < kRopeWarps; ++o) {
+            const int sg = (int)((blockIdx.x * kRopeWarps + o) % (unsigned)p.segs);
+            if ((sg < p.seg_q ? 0 : sg < p.seg_q + p.seg_k ? 1 : 2) == i / D) sum += sm_w[o][i % D];
+        }
+        p.partial[(size_t)blockIdx.x * 2 * D + i] = sum;
+    }
+}
+
+// dqw, dkw [D] = sums of the blocks' parts, in the same order every time.  One block per 32 of the 2 D channels, 32 rows of threads.
+__global__ void __launch_bounds__(1024) rope_weight_grad_kernel(const float* partial, int blocks, int D, float* dqw, float* dkw) {
+    __shared__ float sm[32][33];
+    grid_wait();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, i = blockIdx.x * 32 + x;
+    float sum = 0.f;
+    for (int b = y; b < blocks; b += 32) sum += partial[(size_t)b * 2 * D + i];
+    sm[y][x] = sum;
+    __syncthreads();
+    if (y == 0) {
+        sum = 0.f;
+        for (int r = 0; r < 32; ++r) sum += sm[r][x];
+        float* out = i < D ? dqw : dkw;
+        if (out != nullptr) out[i % D] = sum;
+    }
+}
+
+}  // namespace swaa

@@ -1,0 +1,104 @@
+"""Refusals of the operators around the cache: arguments are looked at on the host, before any device is needed (CPU)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2512_10411_b200 as swaa
+from paper_2512_10411_b200.build import build_library
+
+OK, INVALID, UNSUPPORTED, CUDA, WORKSPACE = 0, -1, -2, -3, -4
+P = 1 << 20  # an aligned address; nothing here gets as far as to use it
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build_library()
+    return swaa.load_library()
+
+
+def needs_device(rc):
+    """What a call with sound arguments gives: it went on to the device, and there is none (or it is a B200 and no case here is run there)."""
+    return rc in (CUDA, UNSUPPORTED)
+
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are not real")
+
+ROPE = dict(q=P, k=P, v=P, q_stride=256, k_stride=128, v_stride=128, q_weight=P, k_weight=P, eps=1e-6, inv_freq=P, rotary_dim=64, interleaved=0,
+            positions=P, T=3, Hq=4, Hkv=2, D=64, q_out=P, k_out=P, v_out=P, stream=None)
+GRAD = dict(q=P, k=P, q_stride=256, k_stride=128, dq_out=P, dk_out=P, dv_out=P, q_weight=P, k_weight=P, eps=1e-6, inv_freq=P, rotary_dim=64,
+            interleaved=0, positions=P, T=3, Hq=4, Hkv=2, D=64, dq=P, dk=P, dv=P, dq_stride=256, dk_stride=128, dv_stride=128, dq_weight=P,
+            dk_weight=P, workspace=P, workspace_bytes=1 << 30, stream=None)
+APPEND = dict(q=P, k=P, v=P, q_stride=256, k_stride=128, v_stride=128, q_weight=P, k_weight=P, eps=1e-6, inv_freq=P, rotary_dim=64, interleaved=0,
+              positions=None, cu=P, seqlens=P, B=2, Tq=3, Lmax=10, Hq=4, Hkv=2, D=64, window=0, n_sink=0, q_out=P, kcache=P, vcache=P, stream=None)
+PAGED = dict(q=P, k=P, v=P, q_stride=256, k_stride=128, v_stride=128, q_weight=P, k_weight=P, eps=1e-6, inv_freq=P, rotary_dim=64, interleaved=0,
+             positions=None, cu=P, seqlens=P, table=P, B=2, Tq=3, max_blocks=4, num_pages=8, page_size=64, Hq=4, Hkv=2, D=64, q_out=P, kpages=P,
+             vpages=P, stream=None)
+
+ROPE_COMMON = [(dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(rotary_dim=80), UNSUPPORTED), (dict(rotary_dim=24), UNSUPPORTED),
+               (dict(rotary_dim=-16), INVALID), (dict(Hq=0), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
+               (dict(inv_freq=None), INVALID), (dict(inv_freq=P + 2), INVALID), (dict(q_weight=P + 1), INVALID), (dict(positions=P + 2), INVALID)]
+
+
+def cases(name, base, extra):
+    return [(name, base, change, want) for change, want in extra]
+
+
+CASES = (
+    cases("swaa_qk_norm_rope", ROPE, ROPE_COMMON + [
+        (dict(T=-1), INVALID), (dict(q=None), INVALID), (dict(k_out=None), INVALID), (dict(positions=None), INVALID), (dict(v_out=None), INVALID),
+        (dict(v=None), INVALID), (dict(q=P + 8), INVALID), (dict(v_out=P + 2), INVALID), (dict(q_stride=252), INVALID), (dict(k_stride=120), INVALID),
+        (dict(v_stride=64), INVALID), (dict(T=0), OK)])
+    + cases("swaa_qk_norm_rope_backward", GRAD, ROPE_COMMON + [
+        (dict(q=None), INVALID), (dict(dq_weight=None), INVALID), (dict(q_weight=None), INVALID), (dict(dv=None), INVALID), (dict(dk=None), INVALID),
+        (dict(dq_stride=250), INVALID), (dict(dv_stride=8), INVALID), (dict(workspace=None), WORKSPACE), (dict(workspace=P + 16), WORKSPACE),
+        (dict(workspace_bytes=8), WORKSPACE), (dict(dk_weight=P + 2), INVALID), (dict(dq=P + 4), INVALID)])
+    + cases("swaa_cache_append", APPEND, ROPE_COMMON + [
+        (dict(B=-1), INVALID), (dict(Lmax=0), INVALID), (dict(window=-1), INVALID), (dict(n_sink=-1), INVALID), (dict(window=9, n_sink=2), INVALID),
+        (dict(window=2 ** 31 - 1, n_sink=2 ** 31 - 1), INVALID), (dict(v=None), INVALID), (dict(cu=None), INVALID), (dict(seqlens=P + 1), INVALID),
+        (dict(kcache=P + 8), INVALID), (dict(v_stride=100), INVALID), (dict(B=0), OK), (dict(Tq=0), OK)])
+    + cases("swaa_cache_append_paged", PAGED, ROPE_COMMON + [
+        (dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED), (dict(page_size=0), INVALID), (dict(num_pages=0), INVALID), (dict(max_blocks=0), INVALID),
+        (dict(max_blocks=2 ** 26), UNSUPPORTED), (dict(vpages=None), INVALID)])
+)
+
+
+@pytest.mark.parametrize("name,base,change,want", CASES, ids=[f"{n}-{c}" for n, _, c, _ in CASES])
+def test_refusals(lib, name, base, change, want):
+    if name.endswith("backward") and want == WORKSPACE and not torch.cuda.is_available():
+        want = CUDA  # how much it needs goes by the device, which is asked for first
+    got = getattr(lib, name)(*{**base, **change}.values())
+    assert got == want, (swaa.status_str(got), swaa.status_str(want))
+
+
+@no_gpu
+@pytest.mark.parametrize("name,base", [("swaa_qk_norm_rope", ROPE), ("swaa_qk_norm_rope_backward", GRAD), ("swaa_cache_append", APPEND), ("swaa_cache_append_paged", PAGED)])
+def test_sound_arguments_get_to_the_device(lib, name, base):
+    assert needs_device(getattr(lib, name)(*base.values()))
+
+
+def test_workspace_sizes_of_refused_shapes(lib):
+    assert swaa.qk_norm_rope_backward_workspace_size(0, 4, 2, 64) == 256
+    assert swaa.qk_norm_rope_backward_workspace_size(10, 4, 2, 80) == 256
+    small, large = (swaa.qk_norm_rope_backward_workspace_size(T, 32, 8, 128) for T in (1, 1 << 20))
+    assert 0 < small <= large < 1 << 22
+
+
+def test_binding_refuses_shapes_and_kinds(lib):
+    x = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    w, pos = torch.ones(64), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(TypeError, match="CUDA"):
+        swaa.swaa_qk_norm_rope(x, x, x, w, w, torch.ones(32), pos, x, x, x)
+    with pytest.raises(ValueError, match="k must be"):
+        swaa.swaa_qk_norm_rope(x, x[:2], None, w, w, torch.ones(32), pos, x, x, None)
+    with pytest.raises(ValueError, match="q_weight must be"):
+        swaa.swaa_qk_norm_rope(x, x, None, w[:32], w, torch.ones(32), pos, x, x, None)
+    with pytest.raises(ValueError, match="positions must be"):
+        swaa.swaa_qk_norm_rope(x, x, None, w, w, torch.ones(32), pos[:2], x, x, None)
+    with pytest.raises(ValueError, match="dq_weight must be"):
+        swaa.swaa_qk_norm_rope_backward(x, x, x, x, None, w, w, torch.ones(32), pos, x, x, None, w[:3], w, None)
+    cu = torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="v is needed"):
+        swaa.swaa_cache_append(x, x, None, w, w, torch.ones(32), cu, cu[:2], x, x, x)
+    with pytest.raises(ValueError, match="seqlens_k"):
+        swaa.swaa_cache_append(x, x, x, w, w, torch.ones(32), cu, cu, x, x, x)
