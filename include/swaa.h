@@ -490,6 +490,41 @@ int swaa_cache_append_paged(const void* q, const void* k, const void* v, long lo
                             const int32_t* block_table, int B, int Tq, int max_blocks, int num_pages, int page_size, int Hq,
                             int Hkv, int D, void* q_out, void* kpages, void* vpages, void* stream);
 
+/*
+ * Eviction by accumulated attention weight (App. A: FA decode retains the cache of the whole context; the trimmed cache below
+ * keeps sinks and window only).  Of every sequence and kv head with more than `budget` entries, the first n_sink and the last
+ * `recent` entries stay, and of the entries between them the budget - n_sink - recent with the largest weights (as
+ * swaa_key_weights and swaa_decode_weighted gather them); among equal weights the entries with the lower index.  NaN counts as larger than
+ * every number, -0 equals 0.  What stays keeps its order and goes to the front of another cache, so that sinks stay first and
+ * recent entries last; sequences of at most `budget` entries are copied as they are.  Attention over the new cache is swaa_decode
+ * with is_full = 1 and seqlens_out; keys keep the rotation of their positions, so later tokens are appended with `positions` given.
+ * An eviction copies the whole budget: let a cache grow by some tens of entries between two of them.
+ *
+ *   kcache, vcache  device, bf16 [B, Lmax, Hkv, D]; or pages [num_pages, page_size, Hkv, D] and a block table [B, max_blocks], page_size
+ *                   a multiple of 64.
+ *   weights         device, float32 [B, Hkv, weights_rows].
+ *   seqlens         device, int32 [B]; 0 <= seqlens[b] <= Lmax (max_blocks * page_size) and <= weights_rows.  Another value is
+ *                   reported as SWAA_ERR_BAD_SEQLENS through the status word; seqlens_out is 0 then and nothing is copied.
+ *   budget          >= 1, n_sink + recent <= budget.
+ *   kcache_out, vcache_out  device, bf16 [B, Lmax_out, Hkv, D], Lmax_out >= budget; or pages of their own size and table.  Rows from
+ *                   the new length on are left as they are.  Dense caches must not overlap the old ones (SWAA_ERR_INVALID_ARG); new pages
+ *                   may come from the same pool, but must be none that the call reads, nor one another.  A page index outside
+ *                   the pool is reported as SWAA_ERR_BAD_SEQLENS and the entries that need it are not copied.
+ *   weights_out     device, float32 [B, Hkv, weights_out_rows], weights_out_rows >= budget: weights of the entries that stay; not overlapping
+ *                   weights.
+ *   kept            device, int32 [B, Hkv, budget]: their index in the old cache, ascending.  Entries of weights_out and kept from the new
+ *                   length on are left as they are.
+ *   seqlens_out     device, int32 [B]: min(seqlens[b], budget); not seqlens itself.
+ */
+int swaa_cache_evict(const void* kcache, const void* vcache, const float* weights, const int32_t* seqlens, int B, int Lmax,
+                     int weights_rows, int Hkv, int D, int budget, int n_sink, int recent, void* kcache_out, void* vcache_out,
+                     int Lmax_out, float* weights_out, int weights_out_rows, int32_t* kept, int32_t* seqlens_out, void* stream);
+int swaa_cache_evict_paged(const void* kpages, const void* vpages, const float* weights, const int32_t* seqlens,
+                           const int32_t* block_table, int B, int max_blocks, int num_pages, int page_size, int weights_rows, int Hkv,
+                           int D, int budget, int n_sink, int recent, void* kpages_out, void* vpages_out,
+                           const int32_t* block_table_out, int max_blocks_out, int num_pages_out, int page_size_out,
+                           float* weights_out, int weights_out_rows, int32_t* kept, int32_t* seqlens_out, void* stream);
+
 /* Static string for a swaa_status value. */
 const char* swaa_status_str(int status);
 /*

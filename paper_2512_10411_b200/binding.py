@@ -145,6 +145,10 @@ def load_library():
     lib.swaa_cache_append.restype = ci
     lib.swaa_cache_append_paged.argtypes = [vp] * 3 + [ll] * 3 + [vp, vp, cf, vp, ci, ci] + [vp] * 4 + [ci] * 8 + [vp] * 4
     lib.swaa_cache_append_paged.restype = ci
+    lib.swaa_cache_evict.argtypes = [vp] * 4 + [ci] * 8 + [vp, vp, ci, vp, ci, vp, vp, vp]
+    lib.swaa_cache_evict.restype = ci
+    lib.swaa_cache_evict_paged.argtypes = [vp] * 5 + [ci] * 10 + [vp] * 3 + [ci] * 3 + [vp, ci, vp, vp, vp]
+    lib.swaa_cache_evict_paged.restype = ci
     lib.swaa_status_str.argtypes = [ci]
     lib.swaa_status_str.restype = ctypes.c_char_p
     lib.swaa_last_device_status.argtypes = [vp]
@@ -726,6 +730,62 @@ def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q,
     rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, block_table.shape[1], num_pages, page_size, Hq,
                                      Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"),
                                      _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def _evict_args(where, kcache, vcache, weights, seqlens, budget, kcache_out, vcache_out, weights_out, kept, seqlens_out):
+    """Sizes of an eviction's arguments, checked: (B, Hkv, D, budget, rows of weights, of weights_out)."""
+    _on_current_device(kcache, where)
+    B, Hkv, D = seqlens.numel(), kcache.shape[2], kcache.shape[3]
+    rows, rows_out = weights.shape[-1], weights_out.shape[-1]
+    for name, t, shp in (("vcache", vcache, kcache.shape), ("kcache_out", kcache_out, (*kcache_out.shape[:2], Hkv, D)),
+                         ("vcache_out", vcache_out, kcache_out.shape), ("weights", weights, (B, Hkv, rows)), ("weights_out", weights_out, (B, Hkv, rows_out)),
+                         ("kept", kept, (B, Hkv, int(budget))), ("seqlens_out", seqlens_out, (B,))):
+        _shaped(t, shp, where, name)
+    return B, Hkv, D, int(budget), rows, rows_out
+
+
+def swaa_cache_evict(kcache, vcache, weights, seqlens, budget: int, n_sink: int, recent: int, kcache_out, vcache_out, weights_out, kept,
+                     seqlens_out, stream=None) -> None:
+    """Forwards to C swaa_cache_evict.  kcache, vcache [B,Lmax,Hkv,D] bf16; weights f32 [B,Hkv,>=seqlens]; seqlens int32 [B]; the first
+    n_sink, the last `recent` and the heaviest of the other entries stay, `budget` in all, and go in order to kcache_out, vcache_out
+    [B,>=budget,Hkv,D] bf16, weights_out f32 [B,Hkv,>=budget]; kept int32 [B,Hkv,budget]: their old index; seqlens_out int32 [B]."""
+    lib = load_library()
+    where = "swaa_cache_evict"
+    B, Hkv, D, budget, rows, rows_out = _evict_args(where, kcache, vcache, weights, seqlens, budget, kcache_out, vcache_out, weights_out, kept,
+                                                    seqlens_out)
+    if kcache.shape[0] != B or kcache_out.shape[0] != B:
+        raise ValueError(f"{where}: caches must be [B, entries, Hkv, D]")
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    rc = lib.swaa_cache_evict(_dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _dev_ptr(weights, f32, "weights"),
+                              _dev_ptr(seqlens, i32, "seqlens"), B, kcache.shape[1], rows, Hkv, D, budget, int(n_sink), int(recent),
+                              _dev_ptr(kcache_out, bf, "kcache_out"), _dev_ptr(vcache_out, bf, "vcache_out"), kcache_out.shape[1],
+                              _dev_ptr(weights_out, f32, "weights_out"), rows_out, _dev_ptr(kept, i32, "kept"), _dev_ptr(seqlens_out, i32, "seqlens_out"),
+                              _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def swaa_cache_evict_paged(kpages, vpages, weights, seqlens, block_table, budget: int, n_sink: int, recent: int, kpages_out, vpages_out,
+                           block_table_out, weights_out, kept, seqlens_out, stream=None) -> None:
+    """Forwards to C swaa_cache_evict_paged: swaa_cache_evict from pages [num_pages,page_size,Hkv,D] bf16 behind block_table int32
+    [B,max_blocks] into pages behind block_table_out (of the same pool or another; none that the call reads)."""
+    lib = load_library()
+    where = "swaa_cache_evict_paged"
+    B, Hkv, D, budget, rows, rows_out = _evict_args(where, kpages, vpages, weights, seqlens, budget, kpages_out, vpages_out, weights_out, kept,
+                                                    seqlens_out)
+    for name, t in (("block_table", block_table), ("block_table_out", block_table_out)):
+        if t.dim() != 2 or t.shape[0] != B:
+            raise ValueError(f"{where}: {name} must be [B, max_blocks]")
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    rc = lib.swaa_cache_evict_paged(_dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"), _dev_ptr(weights, f32, "weights"),
+                                    _dev_ptr(seqlens, i32, "seqlens"), _dev_ptr(block_table, i32, "block_table"), B, block_table.shape[1],
+                                    kpages.shape[0], kpages.shape[1], rows, Hkv, D, budget, int(n_sink), int(recent),
+                                    _dev_ptr(kpages_out, bf, "kpages_out"), _dev_ptr(vpages_out, bf, "vpages_out"),
+                                    _dev_ptr(block_table_out, i32, "block_table_out"), block_table_out.shape[1], kpages_out.shape[0],
+                                    kpages_out.shape[1], _dev_ptr(weights_out, f32, "weights_out"), rows_out, _dev_ptr(kept, i32, "kept"),
+                                    _dev_ptr(seqlens_out, i32, "seqlens_out"), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 

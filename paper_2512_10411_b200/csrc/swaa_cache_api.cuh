@@ -2,6 +2,7 @@
 // Part of the translation unit of swaa_lib.cu, which includes it last.
 #pragma once
 
+#include "swaa_evict.cuh"
 #include "swaa_rope.cuh"
 
 namespace swaa {
@@ -222,4 +223,130 @@ extern "C" int swaa_cache_append_paged(const void* q, const void* k, const void*
     return append_impl(q, k, v, q_stride, k_stride, v_stride, q_weight, k_weight, eps, inv_freq, rotary_dim, interleaved, positions,
                        cu_seqlens_q, seqlens_k, block_table, B, Tq, max_blocks * page_size, max_blocks, num_pages, page_size, Hq, Hkv, D, 0,
                        0, q_out, kpages, vpages, stream);
+}
+
+// ------------------------------------------------------------------------------------------- eviction
+namespace swaa {
+
+static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+// Blocks of a cluster that works on one (sequence, kv head): more while the launch does not fill the SMs and a block still has
+// several thousand weights.
+static int evict_cluster(long long rows, int length, int sms) {
+    int c = 1;
+    while (c < kEvictMaxCluster && 2 * c * rows <= sms && (length + 2 * c - 1) / (2 * c) >= kEvictTile / 2) c *= 2;
+    return c;
+}
+
+static int evict_impl(EvictParams p, int D, bool paged, cudaStream_t st) {
+    if (p.B < 0 || p.rows < 1 || p.weights_rows < 1 || p.Hkv < 1 || p.budget < 1 || p.n_sink < 0 || p.recent < 0 || p.rows_out < 1)
+        return SWAA_ERR_INVALID_ARG;
+    if ((long long)p.n_sink + p.recent > p.budget || p.rows_out < p.budget || p.weights_out_rows < p.budget) return SWAA_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return SWAA_ERR_UNSUPPORTED;
+    if (p.B > 65535 || (long long)p.B * p.Hkv > 0x7fffffffLL / kEvictMaxCluster) return SWAA_ERR_UNSUPPORTED;  // grid dimensions
+    if (p.B == 0) return SWAA_OK;
+    if (!p.k || !p.v || !p.weights || !p.seqlens || !p.k_out || !p.v_out || !p.weights_out || !p.kept || !p.seqlens_out) return SWAA_ERR_INVALID_ARG;
+    if (paged && (!p.block_table || !p.block_table_out)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned16(p.k) || !aligned16(p.v) || !aligned16(p.k_out) || !aligned16(p.v_out)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned4(p.weights) || !aligned4(p.seqlens) || !aligned4(p.block_table) || !aligned4(p.block_table_out) || !aligned4(p.weights_out) ||
+        !aligned4(p.kept) || !aligned4(p.seqlens_out))
+        return SWAA_ERR_INVALID_ARG;
+    const size_t heads = (size_t)p.B * p.Hkv, in = heads * p.rows * D * 2, out = heads * p.rows_out * D * 2;
+    if (!paged && (overlap(p.k, in, p.k_out, out) || overlap(p.v, in, p.v_out, out) || overlap(p.k, in, p.v_out, out) || overlap(p.v, in, p.k_out, out)))
+        return SWAA_ERR_INVALID_ARG;
+    if (overlap(p.weights, heads * p.weights_rows * 4, p.weights_out, heads * p.weights_out_rows * 4) ||
+        overlap(p.seqlens, (size_t)p.B * 4, p.seqlens_out, (size_t)p.B * 4))
+        return SWAA_ERR_INVALID_ARG;
+    DeviceInfo info;
+    int rc = current_sm100(&info);
+    if (rc != SWAA_OK) return rc;
+    const int length = std::min(p.rows, p.weights_rows);
+    const int ranks = evict_cluster((long long)heads, length, info.sm_count);
+    constexpr int kMostKeys = 48 * 1024;
+    p.cap = std::min(((length + ranks - 1) / ranks + kEvictPerThread - 1) / kEvictPerThread * kEvictPerThread, kMostKeys);
+    static std::atomic<bool> attr_done[64];
+    if (ensure_dynamic_smem(evict_select_kernel, kMostKeys * 4, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(heads * ranks));
+    cfg.blockDim = dim3(kEvictThreads);
+    cfg.dynamicSmemBytes = (size_t)p.cap * 4;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, evict_select_kernel, p) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return SWAA_ERR_CUDA;
+    }
+    launch_counter().fetch_add(1, std::memory_order_relaxed);
+    const int per_block = (kGatherThreads / 32) * (32 / (D / 8)) * kGatherRows;
+    const long long blocks = ((long long)std::min(p.budget, length) * p.Hkv + per_block - 1) / per_block;
+    if (blocks > 0x7fffffffLL) return SWAA_ERR_UNSUPPORTED;
+    return launch_overlapped(D == 128 ? evict_gather_kernel<128> : evict_gather_kernel<64>, dim3((unsigned)blocks, (unsigned)p.B), kGatherThreads, 0, st, p);
+}
+
+static EvictParams evict_params(const void* k, const void* v, const float* weights, const int32_t* seqlens, int B, int weights_rows, int Hkv,
+                                int budget, int n_sink, int recent, void* k_out, void* v_out, float* weights_out, int weights_out_rows,
+                                int32_t* kept, int32_t* seqlens_out) {
+    EvictParams p = {};
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.v = static_cast<const __nv_bfloat16*>(v);
+    p.weights = weights;
+    p.seqlens = seqlens;
+    p.B = B;
+    p.weights_rows = weights_rows;
+    p.Hkv = Hkv;
+    p.budget = budget;
+    p.n_sink = n_sink;
+    p.recent = recent;
+    p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.v_out = static_cast<__nv_bfloat16*>(v_out);
+    p.weights_out = weights_out;
+    p.weights_out_rows = weights_out_rows;
+    p.kept = kept;
+    p.seqlens_out = seqlens_out;
+    return p;
+}
+
+}  // namespace swaa
+
+extern "C" int swaa_cache_evict(const void* kcache, const void* vcache, const float* weights, const int32_t* seqlens, int B, int Lmax,
+                                int weights_rows, int Hkv, int D, int budget, int n_sink, int recent, void* kcache_out, void* vcache_out,
+                                int Lmax_out, float* weights_out, int weights_out_rows, int32_t* kept, int32_t* seqlens_out, void* stream) {
+    EvictParams p = evict_params(kcache, vcache, weights, seqlens, B, weights_rows, Hkv, budget, n_sink, recent, kcache_out, vcache_out,
+                                 weights_out, weights_out_rows, kept, seqlens_out);
+    p.rows = Lmax;
+    p.rows_out = Lmax_out;
+    return evict_impl(p, D, false, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int swaa_cache_evict_paged(const void* kpages, const void* vpages, const float* weights, const int32_t* seqlens,
+                                      const int32_t* block_table, int B, int max_blocks, int num_pages, int page_size, int weights_rows,
+                                      int Hkv, int D, int budget, int n_sink, int recent, void* kpages_out, void* vpages_out,
+                                      const int32_t* block_table_out, int max_blocks_out, int num_pages_out, int page_size_out,
+                                      float* weights_out, int weights_out_rows, int32_t* kept, int32_t* seqlens_out, void* stream) {
+    int rc = check_paged_shape(max_blocks, num_pages, page_size);
+    if (rc == SWAA_OK) rc = check_paged_shape(max_blocks_out, num_pages_out, page_size_out);
+    if (rc != SWAA_OK) return rc;
+    EvictParams p = evict_params(kpages, vpages, weights, seqlens, B, weights_rows, Hkv, budget, n_sink, recent, kpages_out, vpages_out,
+                                 weights_out, weights_out_rows, kept, seqlens_out);
+    p.block_table = block_table;
+    p.max_blocks = max_blocks;
+    p.num_pages = num_pages;
+    p.page_size = page_size;
+    p.rows = max_blocks * page_size;
+    p.block_table_out = block_table_out;
+    p.max_blocks_out = max_blocks_out;
+    p.num_pages_out = num_pages_out;
+    p.page_size_out = page_size_out;
+    p.rows_out = max_blocks_out * page_size_out;
+    return evict_impl(p, D, true, reinterpret_cast<cudaStream_t>(stream));
 }

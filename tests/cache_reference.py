@@ -89,3 +89,16 @@ def append(q, k, v, qw, kw, eps, inv_freq, interleaved, cu, seqlens, kc, vc, pos
             at = (b, slot) if table is None else (int(table[b][slot // kc.shape[1]]), slot % kc.shape[1])
             rows[at] = cu[b] + i  # a later token of the call takes the row
     return (*qk_rope(q, qw, eps, pos, inv_freq, interleaved), rows, *qk_rope(k, kw, eps, pos, inv_freq, interleaved))
+
+
+def evict(weights, n, budget, n_sink, recent):
+    """Indices, ascending, of the entries that stay of one row of n weights: the heaviest first, the lower index first among equals; NaN
+    is above every number."""
+    if n <= budget:
+        return list(range(n))
+    j = np.arange(n)
+    held = (j < n_sink) | (j >= n - recent)
+    rest = j[~held]
+    nan = np.isnan(weights[rest])
+    order = np.lexsort((rest, -np.where(nan, 0.0, weights[rest]), ~nan))  # by the last key first
+    return sorted(j[held].tolist() + rest[order[:budget - int(held.sum())]].tolist())

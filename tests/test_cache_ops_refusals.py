@@ -35,6 +35,16 @@ PAGED = dict(q=P, k=P, v=P, q_stride=256, k_stride=128, v_stride=128, q_weight=P
              positions=None, cu=P, seqlens=P, table=P, B=2, Tq=3, max_blocks=4, num_pages=8, page_size=64, Hq=4, Hkv=2, D=64, q_out=P, kpages=P,
              vpages=P, stream=None)
 
+EVICT = dict(k=P, v=P, weights=4 * P, seqlens=5 * P, B=1, Lmax=64, weights_rows=64, Hkv=2, D=64, budget=16, n_sink=4, recent=8, k_out=2 * P, v_out=3 * P,
+             Lmax_out=16, weights_out=6 * P, weights_out_rows=16, kept=7 * P, seqlens_out=8 * P, stream=None)
+EVICT_PAGED = dict(k=P, v=P, weights=4 * P, seqlens=5 * P, table=9 * P, B=1, max_blocks=1, num_pages=3, page_size=64, weights_rows=64, Hkv=2, D=64, budget=16,
+                   n_sink=4, recent=8, k_out=P, v_out=P, table_out=10 * P, max_blocks_out=1, num_pages_out=3, page_size_out=64, weights_out=6 * P,
+                   weights_out_rows=16, kept=7 * P, seqlens_out=8 * P, stream=None)
+EVICT_COMMON = [(dict(B=-1), INVALID), (dict(budget=0, n_sink=0, recent=0), INVALID), (dict(n_sink=9), INVALID), (dict(recent=-1), INVALID),
+                (dict(n_sink=2 ** 31 - 1, recent=2 ** 31 - 1), INVALID), (dict(weights_out_rows=15), INVALID), (dict(D=80), UNSUPPORTED), (dict(B=65536), UNSUPPORTED),
+                (dict(Hkv=0), INVALID), (dict(weights=None), INVALID), (dict(kept=None), INVALID), (dict(kept=7 * P + 1), INVALID), (dict(v=P + 4), INVALID),
+                (dict(weights_out=4 * P + 400), INVALID), (dict(seqlens_out=5 * P), INVALID), (dict(weights_rows=0), INVALID), (dict(B=0), OK)]
+
 ROPE_COMMON = [(dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(rotary_dim=80), UNSUPPORTED), (dict(rotary_dim=24), UNSUPPORTED),
                (dict(rotary_dim=-16), INVALID), (dict(Hq=0), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
                (dict(inv_freq=None), INVALID), (dict(inv_freq=P + 2), INVALID), (dict(q_weight=P + 1), INVALID), (dict(positions=P + 2), INVALID)]
@@ -60,6 +70,8 @@ CASES = (
     + cases("swaa_cache_append_paged", PAGED, ROPE_COMMON + [
         (dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED), (dict(page_size=0), INVALID), (dict(num_pages=0), INVALID), (dict(max_blocks=0), INVALID),
         (dict(max_blocks=2 ** 26), UNSUPPORTED), (dict(vpages=None), INVALID)])
+    + cases("swaa_cache_evict", EVICT, EVICT_COMMON + [(dict(Lmax_out=15), INVALID), (dict(k_out=P + 4096), INVALID), (dict(v_out=P), INVALID), (dict(Lmax=0), INVALID)])
+    + cases("swaa_cache_evict_paged", EVICT_PAGED, EVICT_COMMON + [(dict(table_out=None), INVALID), (dict(page_size_out=16), UNSUPPORTED), (dict(num_pages_out=0), INVALID)])
 )
 
 
@@ -72,7 +84,8 @@ def test_refusals(lib, name, base, change, want):
 
 
 @no_gpu
-@pytest.mark.parametrize("name,base", [("swaa_qk_norm_rope", ROPE), ("swaa_qk_norm_rope_backward", GRAD), ("swaa_cache_append", APPEND), ("swaa_cache_append_paged", PAGED)])
+@pytest.mark.parametrize("name,base", [("swaa_qk_norm_rope", ROPE), ("swaa_qk_norm_rope_backward", GRAD), ("swaa_cache_append", APPEND), ("swaa_cache_append_paged", PAGED),
+                                       ("swaa_cache_evict", EVICT), ("swaa_cache_evict_paged", EVICT_PAGED)])
 def test_sound_arguments_get_to_the_device(lib, name, base):
     assert needs_device(getattr(lib, name)(*base.values()))
 

@@ -49,3 +49,14 @@ def test_gradient_against_differences(interleaved, normed):
 def test_bf16_rounding():
     x = np.array([1.0, 1 + 2.0 ** -8, 1 + 3 * 2.0 ** -8, -3.14159, 0.0])
     np.testing.assert_array_equal(ref.bf16(x), [1.0, 1.0, 1 + 2.0 ** -6, -3.140625, 0.0])
+
+
+def test_eviction_keeps_the_heaviest_in_order():
+    w = np.array([0.0, 5.0, 1.0, 5.0, 0.0, 2.0, 0.5, 9.0])
+    assert ref.evict(w, 8, 8, 0, 0) == list(range(8))
+    assert ref.evict(w, 8, 3, 0, 0) == [1, 3, 7]
+    assert ref.evict(w, 8, 3, 1, 1) == [0, 1, 7]
+    assert ref.evict(w, 6, 4, 0, 2) == [1, 3, 4, 5]
+    assert ref.evict(w, 8, 2, 0, 2) == [6, 7]
+    assert ref.evict(np.array([1.0, np.nan, 3.0, -0.0, 0.0]), 5, 3, 0, 0) == [0, 1, 2]
+    assert ref.evict(np.array([-0.0, 0.0, -1.0, 0.0]), 4, 2, 0, 0) == [0, 1]
