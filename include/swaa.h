@@ -491,6 +491,30 @@ int swaa_cache_append_paged(const void* q, const void* k, const void* v, long lo
                             int Hkv, int D, void* q_out, void* kpages, void* vpages, void* stream);
 
 /*
+ * Decode that also gathers the attention weights of the entries (for swaa_cache_evict): swaa_decode / swaa_decode_paged, and
+ *     weights_out[b, g, j] = weights_in[b, g, j] + sum over the query heads h of kv head g of p(b, h, j)
+ * for every entry j < seqlens[b], p = softmax weights of the row (0 where the mask hides the entry).  The scores are formed once, on the
+ * way to the output; the output is that of swaa_decode, bit for bit.
+ *
+ *   weights_in      device, float32 [B, Hkv, weights_rows]; NULL: zeros; may be weights_out, no other overlap.  The entry of the
+ *                   new token itself, seqlens[b] - 1, starts from 0, whatever weights_in holds there: what appends an entry has
+ *                   nothing to clear.
+ *   weights_out     device, float32 [B, Hkv, weights_rows]; entries from seqlens[b] on are left as they are.  A sequence with more
+ *                   entries than weights_rows is reported as SWAA_ERR_BAD_SEQLENS through the status word and gathers nothing.
+ *   workspace       at least swaa_decode_weighted_workspace_size(...) bytes (paged: Lmax = max_blocks * page_size), 256-byte aligned,
+ *                   uninitialised: the scratch of swaa_decode and 4 bytes per visible entry and query head.
+ * B, Hkv at most 65535.  Other arguments and status codes as for swaa_decode, swaa_decode_paged.
+ */
+size_t swaa_decode_weighted_workspace_size(int B, int Hq, int Hkv, int D, int Lmax, int window, int n_sink, int is_full);
+int swaa_decode_weighted(const void* q, const void* kcache, const void* vcache, void* out, const float* weights_in,
+                         float* weights_out, const int32_t* seqlens, int B, int Lmax, int weights_rows, int Hq, int Hkv, int D,
+                         int window, int n_sink, int is_full, float scale, void* workspace, size_t workspace_bytes, void* stream);
+int swaa_decode_weighted_paged(const void* q, const void* kpages, const void* vpages, void* out, const float* weights_in,
+                               float* weights_out, const int32_t* block_table, const int32_t* seqlens, int B, int max_blocks,
+                               int num_pages, int page_size, int weights_rows, int Hq, int Hkv, int D, int window, int n_sink,
+                               int is_full, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Eviction by accumulated attention weight (App. A: FA decode retains the cache of the whole context; the trimmed cache below
  * keeps sinks and window only).  Of every sequence and kv head with more than `budget` entries, the first n_sink and the last
  * `recent` entries stay, and of the entries between them the budget - n_sink - recent with the largest weights (as

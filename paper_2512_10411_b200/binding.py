@@ -145,6 +145,12 @@ def load_library():
     lib.swaa_cache_append.restype = ci
     lib.swaa_cache_append_paged.argtypes = [vp] * 3 + [ll] * 3 + [vp, vp, cf, vp, ci, ci] + [vp] * 4 + [ci] * 8 + [vp] * 4
     lib.swaa_cache_append_paged.restype = ci
+    lib.swaa_decode_weighted_workspace_size.argtypes = [ci] * 8
+    lib.swaa_decode_weighted_workspace_size.restype = sz
+    lib.swaa_decode_weighted.argtypes = [vp] * 7 + [ci] * 9 + [cf, vp, sz, vp]
+    lib.swaa_decode_weighted.restype = ci
+    lib.swaa_decode_weighted_paged.argtypes = [vp] * 8 + [ci] * 11 + [cf, vp, sz, vp]
+    lib.swaa_decode_weighted_paged.restype = ci
     lib.swaa_cache_evict.argtypes = [vp] * 4 + [ci] * 8 + [vp, vp, ci, vp, ci, vp, vp, vp]
     lib.swaa_cache_evict.restype = ci
     lib.swaa_cache_evict_paged.argtypes = [vp] * 5 + [ci] * 10 + [vp] * 3 + [ci] * 3 + [vp, ci, vp, vp, vp]
@@ -730,6 +736,69 @@ def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q,
     rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, block_table.shape[1], num_pages, page_size, Hq,
                                      Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"),
                                      _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def _weights_rows(where, weights_in, weights_out, B: int, Hkv: int) -> int:
+    """Entries of a row of gathered weights, checked: weights_out f32 [B, Hkv, rows], weights_in the same or None."""
+    if weights_out.dim() != 3:
+        raise ValueError(f"{where}: weights_out must be [B, Hkv, entries]")
+    rows = weights_out.shape[2]
+    _shaped(weights_out, (B, Hkv, rows), where, "weights_out")
+    _shaped(weights_in, (B, Hkv, rows), where, "weights_in")
+    return rows
+
+
+def decode_weighted_workspace_size(B, Hq, Hkv, D, Lmax, window, n_sink, is_full) -> int:
+    """Forwards to C swaa_decode_weighted_workspace_size (bytes).  Lmax of a paged call: max_blocks * page_size."""
+    return int(load_library().swaa_decode_weighted_workspace_size(int(B), int(Hq), int(Hkv), int(D), int(Lmax), int(window), int(n_sink),
+                                                                  int(bool(is_full))))
+
+
+def swaa_decode_weighted(q, kcache, vcache, out, weights_in, weights_out, seqlens, window: int, n_sink: int, is_full: bool, workspace,
+                         scale: float = 0.0, stream=None) -> None:
+    """Forwards to C swaa_decode_weighted: swaa_decode, and weights_out = weights_in + the attention weight of every entry, summed
+    over the query heads of its kv head.  weights_in, weights_out f32 [B,Hkv,>=seqlens] (weights_in may be weights_out, or None for
+    zeros; the new token's own entry starts from 0); workspace: uint8 of decode_weighted_workspace_size(...) bytes."""
+    lib = load_library()
+    where = "swaa_decode_weighted"
+    _on_current_device(q, where)
+    B, Hq, D = q.shape
+    _, Lmax, Hkv, _ = kcache.shape
+    if kcache.shape != (B, Lmax, Hkv, D) or vcache.shape != (B, Lmax, Hkv, D) or out.shape != (B, Hq, D) or seqlens.numel() != B:
+        raise ValueError("swaa_decode_weighted: inconsistent tensor shapes")
+    rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
+    bf, f32 = torch.bfloat16, torch.float32
+    rc = lib.swaa_decode_weighted(_dev_ptr(q, bf, "q"), _dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _dev_ptr(out, bf, "out"),
+                                  _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
+                                  _dev_ptr(seqlens, torch.int32, "seqlens"), B, Lmax, rows, Hq, Hkv, D, int(window), int(n_sink),
+                                  int(bool(is_full)), float(scale), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                  _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def swaa_decode_weighted_paged(q, kpages, vpages, out, weights_in, weights_out, block_table, seqlens, window: int, n_sink: int, is_full: bool,
+                               workspace, scale: float = 0.0, stream=None) -> None:
+    """Forwards to C swaa_decode_weighted_paged: swaa_decode_paged with the weights of swaa_decode_weighted."""
+    lib = load_library()
+    where = "swaa_decode_weighted_paged"
+    _on_current_device(q, where)
+    B, Hq, D = q.shape
+    num_pages, page_size, Hkv, _ = kpages.shape
+    if vpages.shape != kpages.shape or kpages.shape[3] != D or out.shape != (B, Hq, D):
+        raise ValueError("swaa_decode_weighted_paged: inconsistent tensor shapes")
+    if block_table.dim() != 2 or block_table.shape[0] != B or seqlens.numel() != B:
+        raise ValueError("swaa_decode_weighted_paged: block_table must be [B, max_blocks] and seqlens [B]")
+    rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
+    bf, f32 = torch.bfloat16, torch.float32
+    rc = lib.swaa_decode_weighted_paged(_dev_ptr(q, bf, "q"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"), _dev_ptr(out, bf, "out"),
+                                        _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
+                                        _dev_ptr(block_table, torch.int32, "block_table"), _dev_ptr(seqlens, torch.int32, "seqlens"), B,
+                                        block_table.shape[1], num_pages, page_size, rows, Hq, Hkv, D, int(window), int(n_sink),
+                                        int(bool(is_full)), float(scale), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                        _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 

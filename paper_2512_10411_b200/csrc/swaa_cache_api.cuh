@@ -350,3 +350,56 @@ extern "C" int swaa_cache_evict_paged(const void* kpages, const void* vpages, co
     p.rows_out = max_blocks_out * page_size_out;
     return evict_impl(p, D, true, reinterpret_cast<cudaStream_t>(stream));
 }
+
+// -------------------------------------------------------------------------------- decode with weights
+namespace swaa {
+
+static int check_decode_weights(int B, int Lmax, int Hq, int Hkv, const float* in, const float* out, int rows) {
+    if (rows < 1) return SWAA_ERR_INVALID_ARG;
+    if (Lmax > 0x7fffff00) return SWAA_ERR_UNSUPPORTED;  // its tiles, in entries, are counted in an int
+    if (B > 65535 || Hkv > 65535 || Hq / Hkv > 4096) return SWAA_ERR_UNSUPPORTED;  // grid dimensions, shared memory
+    if (B <= 0) return SWAA_OK;
+    const size_t bytes = (size_t)B * Hkv * rows * sizeof(float);
+    if (!out || !aligned4(in) || !aligned4(out) || (in && in != out && overlap(in, bytes, out, bytes))) return SWAA_ERR_INVALID_ARG;
+    return SWAA_OK;
+}
+
+}  // namespace swaa
+
+extern "C" size_t swaa_decode_weighted_workspace_size(int B, int Hq, int Hkv, int D, int Lmax, int window, int n_sink, int is_full) {
+    if (check_decode_shape(B, Hq, Hkv, D, Lmax, window, n_sink, is_full) != SWAA_OK || B == 0 || Lmax > 0x7fffff00) return 256;
+    DeviceInfo info;
+    if (current_device_info(&info) != SWAA_OK) info.sm_count = 148;
+    size_t bytes = 0;
+    for (int paged = 0; paged < 2; ++paged) {
+        const DecodePlan pl = plan_decode(B, Hq, Hkv, D, Lmax, window, n_sink, is_full, info.sm_count, paged != 0);
+        bytes = std::max(bytes, score_plan(pl, B, Hq, Hkv, D, Lmax, window, n_sink, is_full, paged != 0).bytes);
+    }
+    return bytes;
+}
+
+extern "C" int swaa_decode_weighted(const void* q, const void* kcache, const void* vcache, void* out, const float* weights_in,
+                                    float* weights_out, const int32_t* seqlens, int B, int Lmax, int weights_rows, int Hq, int Hkv, int D,
+                                    int window, int n_sink, int is_full, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_decode_shape(B, Hq, Hkv, D, Lmax, window, n_sink, is_full);
+    if (rc == SWAA_OK) rc = check_decode_weights(B, Lmax, Hq, Hkv, weights_in, weights_out, weights_rows);
+    if (rc != SWAA_OK) return rc;
+    const DecodeWeights w = {weights_in, weights_out, weights_rows};
+    return decode_impl(q, kcache, vcache, out, seqlens, nullptr, 0, 0, 0, B, Lmax, Hq, Hkv, D, window, n_sink, is_full, scale, workspace,
+                       workspace_bytes, stream, nullptr, 0, &w);
+}
+
+extern "C" int swaa_decode_weighted_paged(const void* q, const void* kpages, const void* vpages, void* out, const float* weights_in,
+                                          float* weights_out, const int32_t* block_table, const int32_t* seqlens, int B, int max_blocks,
+                                          int num_pages, int page_size, int weights_rows, int Hq, int Hkv, int D, int window, int n_sink,
+                                          int is_full, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_paged_shape(max_blocks, num_pages, page_size);
+    if (rc != SWAA_OK) return rc;
+    if (!block_table) return SWAA_ERR_INVALID_ARG;
+    rc = check_decode_shape(B, Hq, Hkv, D, max_blocks * page_size, window, n_sink, is_full);
+    if (rc == SWAA_OK) rc = check_decode_weights(B, max_blocks * page_size, Hq, Hkv, weights_in, weights_out, weights_rows);
+    if (rc != SWAA_OK) return rc;
+    const DecodeWeights w = {weights_in, weights_out, weights_rows};
+    return decode_impl(q, kpages, vpages, out, seqlens, block_table, max_blocks, num_pages, page_size, B, max_blocks * page_size, Hq, Hkv, D,
+                       window, n_sink, is_full, scale, workspace, workspace_bytes, stream, nullptr, 0, &w);
+}

@@ -61,6 +61,10 @@ struct DecodeParams {
     int pos0;
     float scale;      // softmax scale (natural-log units of the exported maximum)
     float* part_out;  // [B, Hq, D + 2]
+    // attention weights wanted (kScores): raw scores of every visible entry, in the order of an item's tiles, and the rows' sums
+    float* scores;    // [B, Hkv, score_rows, score_heads]
+    float* lse2;      // [B, Hq]: log2 of the sum of 2^(score * sl2)
+    int score_rows, score_heads /* G rounded up to even */;
 };
 
 constexpr int kDecodeTileKeys = 64;
@@ -187,7 +191,7 @@ __device__ __forceinline__ void consumer_sync() {
     asm volatile("bar.sync 1, %0;" ::"n"(kDecodeConsumerThreads) : "memory");
 }
 
-template <int D, int NH, bool kPaged, bool kShard = false>
+template <int D, int NH, bool kPaged, bool kShard = false, bool kScores = false>
 __global__ void __launch_bounds__(kDecodeThreads, 1)
 decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
               const __grid_constant__ CUtensorMap tm_k16, const __grid_constant__ CUtensorMap tm_v16, const DecodeParams p) {
@@ -470,6 +474,17 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ 
 
                 // ---- online softmax over this warp's 16 keys
                 const bool ok0 = g < vw && g >= vb, ok1 = g + 8 < vw && g + 8 >= vb;
+                if (kScores) {
+                    float* row = p.scores + (((size_t)b * p.Hkv + hk) * p.score_rows + (size_t)w.ti * kDecodeTileKeys + 16 * warp + g) * p.score_heads +
+                                 ch * HC + 2 * c;
+#pragma unroll
+                    for (int nh = 0; nh < NH; ++nh) {
+                        if (nh * 8 + 2 * c >= gc) continue;  // (the pair of the last of an odd number of heads ends in the padding)
+                        if (ok0) *reinterpret_cast<float2*>(row + nh * 8) = make_float2(sacc[nh][0], sacc[nh][1]);
+                        if (ok1) *reinterpret_cast<float2*>(row + 8 * p.score_heads + nh * 8) = make_float2(sacc[nh][2], sacc[nh][3]);
+                    }
+                    __syncwarp();
+                }
                 uint32_t pb[NH][2];
 #pragma unroll
                 for (int nh = 0; nh < NH; ++nh) {
@@ -592,6 +607,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ 
                     }
                 } else {
                     p.out[((size_t)b * p.Hq + h0 + hh) * D + d] = __float2bfloat16_rn(den > 0.f ? num / den : 0.f);
+                    if (kScores && d == 0) p.lse2[(size_t)b * p.Hq + h0 + hh] = M * p.sl2 + log2f(den);
                 }
             } else {
                 my_part[hh * (D + 2) + 2 + d] = num;
@@ -685,6 +701,7 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ 
                         } else {
                             const float inv = den > 0.f ? 1.f / den : 0.f;
                             *reinterpret_cast<uint32_t*>(p.out + ((size_t)b * p.Hq + h0 + hh) * D + d) = pack_bf16x2(num0 * inv, num1 * inv);
+                            if (kScores && d == 0) p.lse2[(size_t)b * p.Hq + h0 + hh] = M * p.sl2 + log2f(den);
                         }
                     }
                 };

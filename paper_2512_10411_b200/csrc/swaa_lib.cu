@@ -13,6 +13,7 @@
 #include "swaa.h"
 #include "swaa_internal.cuh"
 #include "swaa_decode.cuh"
+#include "swaa_weights.cuh"
 #include "swaa_prefill.cuh"
 #include "swaa_prefill_token.cuh"
 #include "swaa_backward.cuh"
@@ -251,12 +252,12 @@ static int launch_overlapped(void (*kernel)(P...), dim3 grid, int threads, int s
     return SWAA_OK;
 }
 
-template <int D, int NH, bool kPaged, bool kShard = false>
+template <int D, int NH, bool kPaged, bool kShard = false, bool kScores = false>
 static int launch_decode(const CUtensorMap (&tm)[4], const DecodeParams& p, int blocks, cudaStream_t st) {
     using L = DecodeSmem<D, NH>;
     static std::atomic<bool> attr_done[64];
-    if (ensure_dynamic_smem(decode_kernel<D, NH, kPaged, kShard>, L::kDynamicBytes, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
-    return launch_overlapped(decode_kernel<D, NH, kPaged, kShard>, dim3((unsigned)blocks), kDecodeThreads, L::kDynamicBytes, st, tm[0],
+    if (ensure_dynamic_smem(decode_kernel<D, NH, kPaged, kShard, kScores>, L::kDynamicBytes, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
+    return launch_overlapped(decode_kernel<D, NH, kPaged, kShard, kScores>, dim3((unsigned)blocks), kDecodeThreads, L::kDynamicBytes, st, tm[0],
                              tm[1], tm[2], tm[3], p);
 }
 
@@ -282,12 +283,58 @@ extern "C" int swaa_decode_num_blocks(int B, int Hq, int Hkv, int D, int Lmax, i
 
 namespace swaa {
 
+// Attention weights that a decode call gathers (swaa_decode_weighted), and where its scores stand in the workspace.
+struct DecodeWeights {
+    const float* in;
+    float* out;
+    int rows;
+};
+struct ScorePlan {
+    int rows, heads;  // entries of an item's visible tiles, and floats of each
+    size_t off_lse2, off_scores, bytes;
+};
+static ScorePlan score_plan(const DecodePlan& pl, int B, int Hq, int Hkv, int D, int Lmax, int window, int n_sink, int is_full, bool paged) {
+    ScorePlan s;
+    // one tile more than the longest sequence has, as in plan_decode
+    s.rows = (decode_seq_geom(Lmax, Lmax, window, n_sink, is_full, paged).nt + 1) * kDecodeTileKeys;
+    s.heads = (Hq / Hkv + 1) / 2 * 2;
+    s.off_lse2 = (pl.bytes + 255) / 256 * 256;
+    s.off_scores = s.off_lse2 + ((size_t)B * Hq * sizeof(float) + 255) / 256 * 256;
+    s.bytes = s.off_scores + (size_t)B * Hkv * s.rows * s.heads * sizeof(float);
+    return s;
+}
+
+static int launch_decode_weights(const DecodeParams& d, const DecodeWeights& w, bool paged, cudaStream_t st) {
+    DecodeWeightsParams p;
+    p.scores = d.scores;
+    p.lse2 = d.lse2;
+    p.weights_in = w.in;
+    p.weights_out = w.out;
+    p.seqlens = d.seqlens;
+    p.Lmax = d.Lmax;
+    p.weights_rows = w.rows;
+    p.Hq = d.Hq;
+    p.Hkv = d.Hkv;
+    p.G = d.G;
+    p.score_rows = d.score_rows;
+    p.score_heads = d.score_heads;
+    p.window = d.window;
+    p.n_sink = d.n_sink;
+    p.is_full = d.is_full;
+    p.paged = paged ? 1 : 0;
+    p.sl2 = d.sl2;
+    const int per_block = kDecodeWeightsThreads * kDecodeWeightsKeys;
+    const dim3 grid((unsigned)((std::min(d.Lmax, w.rows) + per_block - 1) / per_block), (unsigned)d.Hkv, (unsigned)d.B);
+    return launch_overlapped(decode_weights_kernel, grid, kDecodeWeightsThreads, d.G * (int)sizeof(float), st, p);
+}
+
 // Shared body of swaa_decode (block_table == nullptr: dense cache [B, Lmax, Hkv, D]) and swaa_decode_paged
 // (cache = pages [num_pages, page_size, Hkv, D]; Lmax = max_blocks * page_size).
 static int decode_impl(const void* q, const void* kcache, const void* vcache, void* out, const int32_t* seqlens,
                        const int32_t* block_table, int max_blocks, int num_pages, int page_size, int B, int Lmax, int Hq,
                        int Hkv, int D, int window, int n_sink, int is_full, float scale, void* workspace,
-                       size_t workspace_bytes, void* stream, float* part_out = nullptr, int pos0 = 0) {
+                       size_t workspace_bytes, void* stream, float* part_out = nullptr, int pos0 = 0,
+                       const DecodeWeights* weights = nullptr) {
     const bool paged = block_table != nullptr;
     const bool shard = part_out != nullptr;  // one shard of a cache cut along the context: `out` is not used
     int rc = check_decode_shape(B, Hq, Hkv, D, Lmax, window, n_sink, is_full);
@@ -304,7 +351,8 @@ static int decode_impl(const void* q, const void* kcache, const void* vcache, vo
     if (info.cc_major != 10) return SWAA_ERR_UNSUPPORTED;
     const DecodePlan pl = plan_decode(B, Hq, Hkv, D, Lmax, window, n_sink, is_full, info.sm_count, paged, shard);
     if (pl.too_large) return SWAA_ERR_UNSUPPORTED;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < pl.bytes)
+    const ScorePlan sp = weights ? score_plan(pl, B, Hq, Hkv, D, Lmax, window, n_sink, is_full, paged) : ScorePlan();
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < (weights ? sp.bytes : pl.bytes))
         return SWAA_ERR_WORKSPACE;
 
     // K, V with the full box; K, V with the small box.  A paged cache is addressed as (page, row in page).
@@ -345,6 +393,19 @@ static int decode_impl(const void* q, const void* kcache, const void* vcache, vo
     p.pos0 = pos0;
     p.scale = sc;
     p.part_out = part_out;
+    if (weights) {
+        p.lse2 = reinterpret_cast<float*>(ws + sp.off_lse2);
+        p.scores = reinterpret_cast<float*>(ws + sp.off_scores);
+        p.score_rows = sp.rows;
+        p.score_heads = sp.heads;
+        if (paged)
+            rc = D == 128 ? (pl.NH == 1 ? launch_decode<128, 1, true, false, true>(tm, p, pl.blocks, st) : launch_decode<128, 2, true, false, true>(tm, p, pl.blocks, st))
+                          : (pl.NH == 1 ? launch_decode<64, 1, true, false, true>(tm, p, pl.blocks, st) : launch_decode<64, 2, true, false, true>(tm, p, pl.blocks, st));
+        else
+            rc = D == 128 ? (pl.NH == 1 ? launch_decode<128, 1, false, false, true>(tm, p, pl.blocks, st) : launch_decode<128, 2, false, false, true>(tm, p, pl.blocks, st))
+                          : (pl.NH == 1 ? launch_decode<64, 1, false, false, true>(tm, p, pl.blocks, st) : launch_decode<64, 2, false, false, true>(tm, p, pl.blocks, st));
+        return rc != SWAA_OK ? rc : launch_decode_weights(p, *weights, paged, st);
+    }
     if (shard) {
         if (D == 128)
             return pl.NH == 1 ? launch_decode<128, 1, false, true>(tm, p, pl.blocks, st)

@@ -102,3 +102,57 @@ def evict(weights, n, budget, n_sink, recent):
     nan = np.isnan(weights[rest])
     order = np.lexsort((rest, -np.where(nan, 0.0, weights[rest]), ~nan))  # by the last key first
     return sorted(j[held].tolist() + rest[order[:budget - int(held.sum())]].tolist())
+
+
+def visible(i, j, window, n_sink, full):
+    return (j <= i) & (full | (j > i - window) | (j < n_sink))
+
+
+def scores(q, k, scale):
+    """(scaled scores [rows, keys], bound of their error): D products of bf16 values, exact in fp32, summed in any order and with any
+    rounding of an fp32 sum, then one product with the scale."""
+    D = q.shape[-1]
+    x = q @ k.T * scale
+    return x, (D + 2) * 2.0 ** -23 * (np.abs(q) @ np.abs(k).T) * scale
+
+
+def softmax_weights(q, k, seen, scale):
+    """(p [rows, keys], bound): softmax over the visible keys of every row.  An exponent is off by the score's and the row's
+    sum's error and by two fp32 roundings of numbers up to their own size in powers of two; the exponential and the logarithm by 4 half
+    steps; the sum of n terms, in any order, by n half steps relative to itself."""
+    x, err = scores(q, k, scale)
+    x = np.where(seen, x, -np.inf)
+    m = x.max(-1, keepdims=True)
+    e = np.exp(x - m)
+    total = e.sum(-1, keepdims=True)
+    p = e / total
+    worst = np.where(seen, err, 0).max(-1, keepdims=True)
+    size = 4 * 1.45 * (np.abs(np.where(seen, x, 0)).max(-1, keepdims=True) + np.log(total) + 4) * U32
+    # below the smallest normal fp32 number, 2^-126, an exponential is 0: the relative error is 1 there, the absolute one below 2^-126
+    return p, p * np.expm1(2 * worst + size + (seen.sum(-1, keepdims=True) + 16) * U32) + 2.0 ** -126
+
+
+def decode_weights(q, k, length, window, n_sink, full, scale):
+    """Weights of the entries of one sequence, [Hkv, length], and their bound: q [Hq, D], k [length, Hkv, D]."""
+    Hq, Hkv = q.shape[0], k.shape[1]
+    G = Hq // Hkv
+    seen = np.broadcast_to(visible(length - 1, np.arange(length), window, n_sink, full), (G, length))
+    got = [softmax_weights(q[g * G:(g + 1) * G], k[:length, g], seen, scale) for g in range(Hkv)]
+    return np.stack([p.sum(0) for p, _ in got]), np.stack([e.sum(0) + (G + 1) * U32 * p.sum(0) for p, e in got])
+
+
+def key_weights(q, k, lse, i, window, n_sink, full, scale):
+    """Weights that the queries at positions i give to the keys 0 .. len(k) - 1 of their sequence, [Hkv, keys], and their bound:
+    q [rows, Hq, D], k [keys, Hkv, D], lse [Hq, rows] (natural logarithm, taken as given)."""
+    Hq, Hkv = q.shape[1], k.shape[1]
+    G, n = Hq // Hkv, k.shape[0]
+    seen = visible(np.asarray(i)[:, None], np.arange(n)[None], window, n_sink, full)
+    out, bound = np.zeros((Hkv, n)), np.zeros((Hkv, n))
+    for h in range(Hq):
+        x, err = scores(q[:, h], k[:, h // G], scale)
+        x = np.where(seen, x, -np.inf) - lse[h][:, None]
+        p = np.exp(x)
+        size = 4 * 1.45 * (np.abs(np.where(seen, x, 0)) + 2 * np.abs(lse[h][:, None]) + 4) * U32
+        out[h // G] += p.sum(0)
+        bound[h // G] += (p * np.expm1(err + size) + 2.0 ** -126).sum(0)  # exponentials below 2^-126 are 0
+    return out, bound + (len(i) * G + 16) * U32 * out

@@ -45,6 +45,14 @@ EVICT_COMMON = [(dict(B=-1), INVALID), (dict(budget=0, n_sink=0, recent=0), INVA
                 (dict(Hkv=0), INVALID), (dict(weights=None), INVALID), (dict(kept=None), INVALID), (dict(kept=7 * P + 1), INVALID), (dict(v=P + 4), INVALID),
                 (dict(weights_out=4 * P + 400), INVALID), (dict(seqlens_out=5 * P), INVALID), (dict(weights_rows=0), INVALID), (dict(B=0), OK)]
 
+DECODE = dict(q=P, k=P, v=P, out=P, weights_in=2 * P, weights_out=3 * P, seqlens=P, B=2, Lmax=64, weights_rows=64, Hq=4, Hkv=2, D=64, window=8, n_sink=4,
+              is_full=1, scale=0.0, workspace=P, workspace_bytes=1 << 30, stream=None)
+DECODE_PAGED = dict(q=P, k=P, v=P, out=P, weights_in=2 * P, weights_out=3 * P, table=P, seqlens=P, B=2, max_blocks=1, num_pages=2, page_size=64, weights_rows=64,
+                    Hq=4, Hkv=2, D=64, window=8, n_sink=4, is_full=1, scale=0.0, workspace=P, workspace_bytes=1 << 30, stream=None)
+DECODE_COMMON = [(dict(weights_out=None), INVALID), (dict(weights_out=2 * P + 64), INVALID), (dict(weights_in=2 * P + 2), INVALID), (dict(weights_rows=0), INVALID),
+                 (dict(B=65536), UNSUPPORTED), (dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(window=0, is_full=0), INVALID), (dict(q=None), INVALID),
+                 (dict(k=P + 8), INVALID), (dict(n_sink=-1), INVALID), (dict(Hq=8194), UNSUPPORTED), (dict(B=0), OK)]
+
 ROPE_COMMON = [(dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(rotary_dim=80), UNSUPPORTED), (dict(rotary_dim=24), UNSUPPORTED),
                (dict(rotary_dim=-16), INVALID), (dict(Hq=0), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
                (dict(inv_freq=None), INVALID), (dict(inv_freq=P + 2), INVALID), (dict(q_weight=P + 1), INVALID), (dict(positions=P + 2), INVALID)]
@@ -70,6 +78,8 @@ CASES = (
     + cases("swaa_cache_append_paged", PAGED, ROPE_COMMON + [
         (dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED), (dict(page_size=0), INVALID), (dict(num_pages=0), INVALID), (dict(max_blocks=0), INVALID),
         (dict(max_blocks=2 ** 26), UNSUPPORTED), (dict(vpages=None), INVALID)])
+    + cases("swaa_decode_weighted", DECODE, DECODE_COMMON + [(dict(Lmax=2 ** 31 - 1), UNSUPPORTED), (dict(Lmax=0), INVALID)])
+    + cases("swaa_decode_weighted_paged", DECODE_PAGED, DECODE_COMMON + [(dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED)])
     + cases("swaa_cache_evict", EVICT, EVICT_COMMON + [(dict(Lmax_out=15), INVALID), (dict(k_out=P + 4096), INVALID), (dict(v_out=P), INVALID), (dict(Lmax=0), INVALID)])
     + cases("swaa_cache_evict_paged", EVICT_PAGED, EVICT_COMMON + [(dict(table_out=None), INVALID), (dict(page_size_out=16), UNSUPPORTED), (dict(num_pages_out=0), INVALID)])
 )
@@ -85,7 +95,8 @@ def test_refusals(lib, name, base, change, want):
 
 @no_gpu
 @pytest.mark.parametrize("name,base", [("swaa_qk_norm_rope", ROPE), ("swaa_qk_norm_rope_backward", GRAD), ("swaa_cache_append", APPEND), ("swaa_cache_append_paged", PAGED),
-                                       ("swaa_cache_evict", EVICT), ("swaa_cache_evict_paged", EVICT_PAGED)])
+                                       ("swaa_cache_evict", EVICT), ("swaa_cache_evict_paged", EVICT_PAGED), ("swaa_decode_weighted", DECODE),
+                                       ("swaa_decode_weighted_paged", DECODE_PAGED)])
 def test_sound_arguments_get_to_the_device(lib, name, base):
     assert needs_device(getattr(lib, name)(*base.values()))
 
