@@ -491,6 +491,40 @@ int swaa_cache_append_paged(const void* q, const void* k, const void* v, long lo
                             int Hkv, int D, void* q_out, void* kpages, void* vpages, void* stream);
 
 /*
+ * Attention weights that the keys of a prompt receive (for swaa_cache_evict), from the log-sum-exp rows that the prefill calls
+ * write:
+ *     weights_out[b, g, j] = weights_in[b, g, j] + sum over queries i and query heads h of kv head g of exp(scale q_ih . k_j - lse_ih)
+ * over the pairs that the mask lets see each other, for every key j < len_k of sequence b (0 is added where no query sees it).  The batch
+ * is described as in swaa_prefill_chunked: the queries of a sequence are the last len_q of its len_k tokens; with len_q == len_k
+ * for every sequence it is that of swaa_prefill.  Chunks of a prompt are gathered one call after another.
+ *
+ *   q               device, bf16 [Tq, Hq, D], packed by cu_seqlens_q
+ *   k               device, bf16 [Tk, Hkv, D], packed by cu_seqlens_k; or pages [num_pages, page_size, Hkv, D] with a block table,
+ *                   page_size a multiple of 128, as in swaa_prefill_paged
+ *   lse             device, float32 [Hq, Tq], of the attention whose weights are wanted (same keys, mask and scale)
+ *   weights_in      device, float32 [B, Hkv, weights_rows]; NULL: zeros; may be weights_out, no other overlap.  Entries of the call's
+ *                   own tokens (the last len_q) start from 0, whatever weights_in holds there.
+ *   weights_out     device, float32 [B, Hkv, weights_rows]; entries from len_k on are left as they are.
+ *   last            > 0: only the last `last` queries of every sequence count (what the end of a prompt looks at); 0: all.
+ *   workspace       at least swaa_key_weights_workspace_size(...) bytes (paged: max_seqlen_k = the smaller of max_blocks * page_size and
+ *                   weights_rows), 256-byte aligned, uninitialised: sums of blocks that share the queries of a key.
+ * A sequence with len_q > len_k, longer than the stated bounds or than weights_rows is reported as SWAA_ERR_BAD_SEQLENS through the
+ * status word and gathers nothing; a page index outside [0, num_pages) likewise, for its keys.  Sums are taken in a fixed order.  Other
+ * arguments and status codes as for swaa_prefill_chunked and swaa_prefill_paged.
+ */
+size_t swaa_key_weights_workspace_size(int B, int max_seqlen_q, int max_seqlen_k, int Hq, int Hkv, int window, int n_sink,
+                                       int is_full, int last);
+int swaa_key_weights(const void* q, const void* k, const float* lse, const float* weights_in, float* weights_out,
+                     const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int B, int Tq, int Tk, int max_seqlen_q,
+                     int max_seqlen_k, int weights_rows, int Hq, int Hkv, int D, int window, int n_sink, int is_full, float scale,
+                     int last, void* workspace, size_t workspace_bytes, void* stream);
+int swaa_key_weights_paged(const void* q, const void* kpages, const float* lse, const float* weights_in, float* weights_out,
+                           const int32_t* cu_seqlens_q, const int32_t* seqlens_k, const int32_t* block_table, int B, int Tq,
+                           int max_seqlen_q, int max_blocks, int num_pages, int page_size, int weights_rows, int Hq, int Hkv, int D,
+                           int window, int n_sink, int is_full, float scale, int last, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
  * Decode that also gathers the attention weights of the entries (for swaa_cache_evict): swaa_decode / swaa_decode_paged, and
  *     weights_out[b, g, j] = weights_in[b, g, j] + sum over the query heads h of kv head g of p(b, h, j)
  * for every entry j < seqlens[b], p = softmax weights of the row (0 where the mask hides the entry).  The scores are formed once, on the

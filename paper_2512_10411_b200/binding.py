@@ -151,6 +151,12 @@ def load_library():
     lib.swaa_decode_weighted.restype = ci
     lib.swaa_decode_weighted_paged.argtypes = [vp] * 8 + [ci] * 11 + [cf, vp, sz, vp]
     lib.swaa_decode_weighted_paged.restype = ci
+    lib.swaa_key_weights_workspace_size.argtypes = [ci] * 9
+    lib.swaa_key_weights_workspace_size.restype = sz
+    lib.swaa_key_weights.argtypes = [vp] * 7 + [ci] * 12 + [cf, ci, vp, sz, vp]
+    lib.swaa_key_weights.restype = ci
+    lib.swaa_key_weights_paged.argtypes = [vp] * 8 + [ci] * 13 + [cf, ci, vp, sz, vp]
+    lib.swaa_key_weights_paged.restype = ci
     lib.swaa_cache_evict.argtypes = [vp] * 4 + [ci] * 8 + [vp, vp, ci, vp, ci, vp, vp, vp]
     lib.swaa_cache_evict.restype = ci
     lib.swaa_cache_evict_paged.argtypes = [vp] * 5 + [ci] * 10 + [vp] * 3 + [ci] * 3 + [vp, ci, vp, vp, vp]
@@ -748,6 +754,64 @@ def _weights_rows(where, weights_in, weights_out, B: int, Hkv: int) -> int:
     _shaped(weights_out, (B, Hkv, rows), where, "weights_out")
     _shaped(weights_in, (B, Hkv, rows), where, "weights_in")
     return rows
+
+
+def key_weights_workspace_size(B, max_seqlen_q, max_seqlen_k, Hq, Hkv, window, n_sink, is_full, last=0) -> int:
+    """Forwards to C swaa_key_weights_workspace_size (bytes).  max_seqlen_k of a paged call: the smaller of max_blocks * page_size and
+    the entries of weights_out."""
+    return int(load_library().swaa_key_weights_workspace_size(int(B), int(max_seqlen_q), int(max_seqlen_k), int(Hq), int(Hkv), int(window),
+                                                              int(n_sink), int(bool(is_full)), int(last)))
+
+
+def swaa_key_weights(q, k, lse, weights_in, weights_out, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_seqlen_k: int, window: int,
+                     n_sink: int, is_full: bool, workspace, last: int = 0, scale: float = 0.0, stream=None) -> None:
+    """Forwards to C swaa_key_weights: weights_out = weights_in + the attention weight that every key receives from the queries of the
+    call (with last > 0: from the last `last` of each sequence), summed over the query heads of its kv head.  q [Tq,Hq,D]; k
+    [Tk,Hkv,D] bf16; lse f32 [Hq,Tq] as the prefill calls write it; weights_in, weights_out f32 [B,Hkv,>=len_k] (weights_in may be
+    weights_out, or None for zeros; entries of the call's own tokens start from 0); workspace: uint8 of key_weights_workspace_size(...)."""
+    lib = load_library()
+    where = "swaa_key_weights"
+    _on_current_device(q, where)
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[0], k.shape[1]
+    B = cu_seqlens_q.numel() - 1
+    if k.shape != (Tk, Hkv, D) or cu_seqlens_k.numel() != B + 1:
+        raise ValueError("swaa_key_weights: inconsistent tensor shapes")
+    _shaped(lse, (Hq, Tq), where, "lse")
+    rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    rc = lib.swaa_key_weights(_dev_ptr(q, bf, "q"), _dev_ptr(k, bf, "k"), _dev_ptr(lse, f32, "lse"), _dev_ptr(weights_in, f32, "weights_in"),
+                              _dev_ptr(weights_out, f32, "weights_out"), _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"),
+                              _dev_ptr(cu_seqlens_k, i32, "cu_seqlens_k"), B, Tq, Tk, int(max_seqlen_q), int(max_seqlen_k), rows, Hq, Hkv, D,
+                              int(window), int(n_sink), int(bool(is_full)), float(scale), int(last), _dev_ptr(workspace, torch.uint8, "workspace"),
+                              workspace.numel(), _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
+
+
+def swaa_key_weights_paged(q, kpages, lse, weights_in, weights_out, cu_seqlens_q, seqlens_k, block_table, max_seqlen_q: int, window: int,
+                           n_sink: int, is_full: bool, workspace, last: int = 0, scale: float = 0.0, stream=None) -> None:
+    """Forwards to C swaa_key_weights_paged: swaa_key_weights with the keys in kpages [num_pages,page_size,Hkv,D] bf16 behind
+    block_table int32 [B,max_blocks], seqlens_k int32 [B] of them."""
+    lib = load_library()
+    where = "swaa_key_weights_paged"
+    _on_current_device(q, where)
+    Tq, Hq, D = q.shape
+    num_pages, page_size, Hkv, _ = kpages.shape
+    B = cu_seqlens_q.numel() - 1
+    if kpages.shape[3] != D or block_table.dim() != 2 or block_table.shape[0] != B or seqlens_k.numel() != B:
+        raise ValueError("swaa_key_weights_paged: inconsistent tensor shapes")
+    _shaped(lse, (Hq, Tq), where, "lse")
+    rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
+    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    rc = lib.swaa_key_weights_paged(_dev_ptr(q, bf, "q"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(lse, f32, "lse"),
+                                    _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
+                                    _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k"),
+                                    _dev_ptr(block_table, i32, "block_table"), B, Tq, int(max_seqlen_q), block_table.shape[1], num_pages, page_size,
+                                    rows, Hq, Hkv, D, int(window), int(n_sink), int(bool(is_full)), float(scale), int(last),
+                                    _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream_ptr(stream))
+    if rc != SWAA_OK:
+        raise SwaaError(rc, where)
 
 
 def decode_weighted_workspace_size(B, Hq, Hkv, D, Lmax, window, n_sink, is_full) -> int:

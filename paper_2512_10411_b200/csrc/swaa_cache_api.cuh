@@ -403,3 +403,149 @@ extern "C" int swaa_decode_weighted_paged(const void* q, const void* kpages, con
     return decode_impl(q, kpages, vpages, out, seqlens, block_table, max_blocks, num_pages, page_size, B, max_blocks * page_size, Hq, Hkv, D,
                        window, n_sink, is_full, scale, workspace, workspace_bytes, stream, nullptr, 0, &w);
 }
+
+// ----------------------------------------------------------------------------------- weights of a prompt
+namespace swaa {
+
+// Launch shape and workspace: chunks of the key tiles, [chunks of all tiles | chunks of the tiles that hold sinks].
+struct KeyWeightsPlan {
+    int key_tiles, chunks, sink_tiles, sink_chunks;
+    size_t off_sink, bytes;
+};
+static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int Hkv, int window, int n_sink, bool full, int last) {
+    KeyWeightsPlan pl;
+    const long long rows = last > 0 && last < max_q ? last : max_q;
+    const long long most = (rows + kKeyWeightsRows - 1) / kKeyWeightsRows;  // query tiles of a sequence
+    // a key tile meets the queries of `window + 127` positions, which start anywhere in a tile
+    const long long band = full ? most : std::min(most, ((long long)window + kKeyWeightsKeys - 1) / kKeyWeightsRows + 2);
+    auto chunks = [](long long tiles) { return (int)std::max(1ll, (tiles + kKeyWeightsChunk - 1) / kKeyWeightsChunk); };
+    pl.key_tiles = (int)(((long long)max_k + kKeyWeightsKeys - 1) / kKeyWeightsKeys);
+    pl.chunks = chunks(band);
+    pl.sink_chunks = full ? 1 : chunks(most);
+    pl.sink_tiles = pl.sink_chunks > pl.chunks ? (int)std::min<long long>(((long long)n_sink + kKeyWeightsKeys - 1) / kKeyWeightsKeys, pl.key_tiles) : 0;
+    const size_t tile = (size_t)B * Hkv * kKeyWeightsKeys * sizeof(float);
+    pl.off_sink = pl.chunks > 1 ? tile * pl.chunks * pl.key_tiles : 0;
+    pl.bytes = std::max(pl.off_sink + tile * pl.sink_chunks * pl.sink_tiles, (size_t)256);
+    return pl;
+}
+
+static int check_key_weights(int B, int max_q, int max_k, int Hq, int Hkv, int window, int n_sink, int is_full, int last) {
+    if (B < 0 || max_q < 0 || max_k < 0 || Hq < 1 || Hkv < 1 || n_sink < 0 || last < 0) return SWAA_ERR_INVALID_ARG;
+    if (!is_full && window < 1) return SWAA_ERR_INVALID_ARG;
+    if (Hq % Hkv != 0) return SWAA_ERR_UNSUPPORTED;
+    if ((long long)B * Hkv > 0x7fffffffLL || max_k > 0x7fffff00) return SWAA_ERR_UNSUPPORTED;  // grid, positions of a tile
+    return SWAA_OK;
+}
+
+template <int D>
+static int launch_key_weights(const CUtensorMap& tq, const CUtensorMap& tk, const KeyWeightsParams& p, cudaStream_t st) {
+    using L = KeyWeightsSmem<D>;
+    static std::atomic<bool> attr_done[64];
+    if (ensure_dynamic_smem(key_weights_kernel<D>, L::kBytes, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
+    const long long slots = (long long)p.sink_tiles * p.sink_chunks + (long long)p.key_tiles * p.chunks;
+    auto grid = [&](long long n) {
+        const unsigned y = n < 32768 ? (unsigned)n : 32768u;
+        return dim3((unsigned)(p.B * p.Hkv), y, (unsigned)((n + y - 1) / y));
+    };
+    if (slots > 32768ll * 65535) return SWAA_ERR_UNSUPPORTED;
+    const int rc = launch_overlapped(key_weights_kernel<D>, grid(slots), kKeyWeightsThreads, L::kBytes, st, tq, tk, p);
+    if (rc != SWAA_OK || (p.chunks == 1 && p.sink_tiles == 0)) return rc;
+    return launch_overlapped(key_weights_join_kernel, grid(p.chunks > 1 ? p.key_tiles : p.sink_tiles), kKeyWeightsKeys, 0, st, p);
+}
+
+static int key_weights_impl(const void* q, const void* k, const float* lse, const float* weights_in, float* weights_out, const int32_t* cu_q,
+                            const int32_t* cu_k, const int32_t* seqlens_k, const PagedKV& paged, int B, int Tq, int Tk, int max_q, int max_k,
+                            int weights_rows, int Hq, int Hkv, int D, int window, int n_sink, int is_full, float scale, int last,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_key_weights(B, max_q, max_k, Hq, Hkv, window, n_sink, is_full, last);
+    if (rc != SWAA_OK) return rc;
+    if (Tq < 0 || Tk < 0 || weights_rows < 1) return SWAA_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return SWAA_ERR_UNSUPPORTED;
+    if (B == 0 || max_k == 0) return SWAA_OK;
+    if (!cu_q || !weights_out || (Tq > 0 && (!q || !lse)) || (Tk > 0 && !k)) return SWAA_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned4(lse) || !aligned4(weights_in) || !aligned4(weights_out) || !aligned4(cu_q) || !aligned4(cu_k) ||
+        !aligned4(seqlens_k) || !aligned4(paged.block_table))
+        return SWAA_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)B * Hkv * weights_rows * sizeof(float);
+    if (weights_in && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes)) return SWAA_ERR_INVALID_ARG;
+    const KeyWeightsPlan pl = key_weights_plan(B, max_q, max_k, Hkv, window, n_sink, is_full != 0, last);
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < pl.bytes) return SWAA_ERR_WORKSPACE;
+    DeviceInfo info;
+    if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
+    CUtensorMap tq = {}, tk = {};
+    if (Tq > 0 && (rc = make_token_major_map(&tq, q, Tq, Hq, D, kKeyWeightsRows)) != SWAA_OK) return rc;
+    if (Tk > 0) {
+        rc = cu_k != nullptr ? make_token_major_map(&tk, k, Tk, Hkv, D, kKeyWeightsKeys)
+                             : make_cache_map(&tk, k, paged.num_pages, paged.page_size, Hkv, D, kKeyWeightsKeys);
+        if (rc != SWAA_OK) return rc;
+    }
+    KeyWeightsParams p = {};
+    p.lse = lse;
+    p.weights_in = weights_in;
+    p.weights_out = weights_out;
+    p.cu_q = cu_q;
+    p.cu_k = cu_k;
+    p.seqlens_k = seqlens_k;
+    p.block_table = paged.block_table;
+    p.max_blocks = paged.max_blocks;
+    p.page_size = paged.page_size;
+    p.num_pages = paged.num_pages;
+    p.B = B;
+    p.Tq = Tq;
+    p.Tk = Tk;
+    p.max_q = max_q;
+    p.max_k = max_k;
+    p.weights_rows = weights_rows;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.G = Hq / Hkv;
+    p.window = window;
+    p.n_sink = n_sink;
+    p.is_full = is_full ? 1 : 0;
+    p.last = last;
+    p.sl2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    p.key_tiles = pl.key_tiles;
+    p.chunks = pl.chunks;
+    p.sink_tiles = pl.sink_tiles;
+    p.sink_chunks = pl.sink_chunks;
+    p.part = static_cast<float*>(workspace);
+    p.sink_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_sink);
+    cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    return D == 128 ? launch_key_weights<128>(tq, tk, p, st) : launch_key_weights<64>(tq, tk, p, st);
+}
+
+}  // namespace swaa
+
+extern "C" size_t swaa_key_weights_workspace_size(int B, int max_seqlen_q, int max_seqlen_k, int Hq, int Hkv, int window, int n_sink,
+                                                  int is_full, int last) {
+    if (check_key_weights(B, max_seqlen_q, max_seqlen_k, Hq, Hkv, window, n_sink, is_full, last) != SWAA_OK || B == 0) return 256;
+    return key_weights_plan(B, max_seqlen_q, max_seqlen_k, Hkv, window, n_sink, is_full != 0, last).bytes;
+}
+
+extern "C" int swaa_key_weights(const void* q, const void* k, const float* lse, const float* weights_in, float* weights_out,
+                                const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_k, int B, int Tq, int Tk, int max_seqlen_q,
+                                int max_seqlen_k, int weights_rows, int Hq, int Hkv, int D, int window, int n_sink, int is_full, float scale,
+                                int last, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!cu_seqlens_k && B > 0) return SWAA_ERR_INVALID_ARG;
+    return key_weights_impl(q, k, lse, weights_in, weights_out, cu_seqlens_q, cu_seqlens_k, nullptr, PagedKV(), B, Tq, Tk, max_seqlen_q,
+                            max_seqlen_k, weights_rows, Hq, Hkv, D, window, n_sink, is_full, scale, last, workspace, workspace_bytes, stream);
+}
+
+extern "C" int swaa_key_weights_paged(const void* q, const void* kpages, const float* lse, const float* weights_in, float* weights_out,
+                                      const int32_t* cu_seqlens_q, const int32_t* seqlens_k, const int32_t* block_table, int B, int Tq,
+                                      int max_seqlen_q, int max_blocks, int num_pages, int page_size, int weights_rows, int Hq, int Hkv, int D,
+                                      int window, int n_sink, int is_full, float scale, int last, void* workspace, size_t workspace_bytes,
+                                      void* stream) {
+    const int rc = check_paged_shape(max_blocks, num_pages, page_size);
+    if (rc != SWAA_OK) return rc;
+    if (page_size % kKeyWeightsKeys != 0) return SWAA_ERR_UNSUPPORTED;
+    if (!block_table || (!seqlens_k && B > 0)) return SWAA_ERR_INVALID_ARG;
+    PagedKV paged;
+    paged.block_table = block_table;
+    paged.max_blocks = max_blocks;
+    paged.num_pages = num_pages;
+    paged.page_size = page_size;
+    const int max_k = std::min(max_blocks * page_size, weights_rows);  // longer sequences have no room for their weights
+    return key_weights_impl(q, kpages, lse, weights_in, weights_out, cu_seqlens_q, nullptr, seqlens_k, paged, B, Tq, 1, max_seqlen_q, max_k,
+                            weights_rows, Hq, Hkv, D, window, n_sink, is_full, scale, last, workspace, workspace_bytes, stream);
+}

@@ -53,6 +53,17 @@ DECODE_COMMON = [(dict(weights_out=None), INVALID), (dict(weights_out=2 * P + 64
                  (dict(B=65536), UNSUPPORTED), (dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(window=0, is_full=0), INVALID), (dict(q=None), INVALID),
                  (dict(k=P + 8), INVALID), (dict(n_sink=-1), INVALID), (dict(Hq=8194), UNSUPPORTED), (dict(B=0), OK)]
 
+WEIGHTS = dict(q=P, k=P, lse=P, weights_in=2 * P, weights_out=3 * P, cu_q=P, cu_k=P, B=2, Tq=10, Tk=20, max_q=5, max_k=10, weights_rows=64, Hq=4, Hkv=2, D=64,
+               window=8, n_sink=4, is_full=0, scale=0.0, last=0, workspace=P, workspace_bytes=1 << 30, stream=None)
+WEIGHTS_PAGED = dict(q=P, k=P, lse=P, weights_in=2 * P, weights_out=3 * P, cu_q=P, seqlens_k=P, table=P, B=2, Tq=10, max_q=5, max_blocks=2, num_pages=3,
+                     page_size=128, weights_rows=64, Hq=4, Hkv=2, D=64, window=8, n_sink=4, is_full=0, scale=0.0, last=0, workspace=P, workspace_bytes=1 << 30,
+                     stream=None)
+WEIGHTS_COMMON = [(dict(weights_out=None), INVALID), (dict(weights_out=2 * P + 64), INVALID), (dict(weights_in=2 * P + 2), INVALID), (dict(weights_rows=0), INVALID),
+                  (dict(last=-1), INVALID), (dict(window=0), INVALID), (dict(n_sink=-1), INVALID), (dict(max_q=-1), INVALID), (dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED),
+                  (dict(lse=None), INVALID), (dict(lse=P + 2), INVALID), (dict(q=P + 8), INVALID), (dict(k=None), INVALID), (dict(cu_q=None), INVALID),
+                  (dict(workspace=None), WORKSPACE), (dict(workspace=P + 128), WORKSPACE), (dict(workspace_bytes=8), WORKSPACE), (dict(B=-1), INVALID),
+                  (dict(B=2 ** 30), UNSUPPORTED)]
+
 ROPE_COMMON = [(dict(D=96), UNSUPPORTED), (dict(Hq=5), UNSUPPORTED), (dict(rotary_dim=80), UNSUPPORTED), (dict(rotary_dim=24), UNSUPPORTED),
                (dict(rotary_dim=-16), INVALID), (dict(Hq=0), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID),
                (dict(inv_freq=None), INVALID), (dict(inv_freq=P + 2), INVALID), (dict(q_weight=P + 1), INVALID), (dict(positions=P + 2), INVALID)]
@@ -78,6 +89,9 @@ CASES = (
     + cases("swaa_cache_append_paged", PAGED, ROPE_COMMON + [
         (dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED), (dict(page_size=0), INVALID), (dict(num_pages=0), INVALID), (dict(max_blocks=0), INVALID),
         (dict(max_blocks=2 ** 26), UNSUPPORTED), (dict(vpages=None), INVALID)])
+    + cases("swaa_key_weights", WEIGHTS, WEIGHTS_COMMON + [(dict(cu_k=None), INVALID), (dict(max_k=-1), INVALID), (dict(Tk=-1), INVALID), (dict(B=0), OK),
+                                                           (dict(max_k=0), OK), (dict(max_k=2 ** 31 - 1), UNSUPPORTED)])
+    + cases("swaa_key_weights_paged", WEIGHTS_PAGED, WEIGHTS_COMMON + [(dict(table=None), INVALID), (dict(page_size=64), UNSUPPORTED), (dict(seqlens_k=None), INVALID)])
     + cases("swaa_decode_weighted", DECODE, DECODE_COMMON + [(dict(Lmax=2 ** 31 - 1), UNSUPPORTED), (dict(Lmax=0), INVALID)])
     + cases("swaa_decode_weighted_paged", DECODE_PAGED, DECODE_COMMON + [(dict(table=None), INVALID), (dict(page_size=32), UNSUPPORTED)])
     + cases("swaa_cache_evict", EVICT, EVICT_COMMON + [(dict(Lmax_out=15), INVALID), (dict(k_out=P + 4096), INVALID), (dict(v_out=P), INVALID), (dict(Lmax=0), INVALID)])
@@ -95,7 +109,7 @@ def test_refusals(lib, name, base, change, want):
 
 @no_gpu
 @pytest.mark.parametrize("name,base", [("swaa_qk_norm_rope", ROPE), ("swaa_qk_norm_rope_backward", GRAD), ("swaa_cache_append", APPEND), ("swaa_cache_append_paged", PAGED),
-                                       ("swaa_cache_evict", EVICT), ("swaa_cache_evict_paged", EVICT_PAGED), ("swaa_decode_weighted", DECODE),
+                                       ("swaa_cache_evict", EVICT), ("swaa_cache_evict_paged", EVICT_PAGED), ("swaa_key_weights", WEIGHTS), ("swaa_key_weights_paged", WEIGHTS_PAGED), ("swaa_decode_weighted", DECODE),
                                        ("swaa_decode_weighted_paged", DECODE_PAGED)])
 def test_sound_arguments_get_to_the_device(lib, name, base):
     assert needs_device(getattr(lib, name)(*base.values()))
@@ -126,3 +140,14 @@ def test_binding_refuses_shapes_and_kinds(lib):
         swaa.swaa_cache_append(x, x, None, w, w, torch.ones(32), cu, cu[:2], x, x, x)
     with pytest.raises(ValueError, match="seqlens_k"):
         swaa.swaa_cache_append(x, x, x, w, w, torch.ones(32), cu, cu, x, x, x)
+
+
+def test_key_weights_workspace_grows_with_what_is_cut(lib):
+    """Chunks of 32 query tiles of 64: nothing is cut up to 2048 queries; under a window the sinks' tiles alone are."""
+    size = swaa.key_weights_workspace_size
+    assert size(3, 2048, 9000, 8, 2, 1, 0, True) == 256
+    assert size(3, 2049, 9000, 8, 2, 1, 0, True) == 2 * 3 * 2 * 71 * 128 * 4
+    assert size(3, 9000, 9000, 8, 2, 1000, 0, False) == 256
+    assert size(3, 9000, 9000, 8, 2, 1000, 4, False) == 5 * 3 * 2 * 128 * 4
+    assert size(3, 9000, 9000, 8, 2, 1000, 4, False, last=64) == 256
+    assert size(0, 9000, 9000, 8, 2, 1000, 4, False) == 256
