@@ -35,7 +35,7 @@ static unsigned rope_blocks(int T, int segs, int sms, int per_sm) {
     return (unsigned)std::min(((long long)T * segs + kRopeWarps - 1) / kRopeWarps, most);
 }
 
-constexpr int kRopeBlocksPerSm = 3, kRopeBwdBlocksPerSm = 2;
+constexpr int kRopeBlocksPerSm = 2, kRopeBwdBlocksPerSm = 2;
 
 template <bool kCache>
 static int launch_rope(const RopeParams& p, int D, bool pairs, int sms, cudaStream_t st) {
@@ -442,11 +442,12 @@ static int launch_key_weights(const CUtensorMap& tq, const CUtensorMap& tk, cons
     using L = KeyWeightsSmem<D>;
     static std::atomic<bool> attr_done[64];
     if (ensure_dynamic_smem(key_weights_kernel<D>, L::kBytes, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
-    const long long slots = (long long)p.sink_tiles * p.sink_chunks + (long long)p.key_tiles * p.chunks;
+    long long slots = (long long)p.sink_tiles * p.sink_chunks + (long long)p.key_tiles * p.chunks;
     auto grid = [&](long long n) {
         const unsigned y = n < 32768 ? (unsigned)n : 32768u;
         return dim3((unsigned)(p.B * p.Hkv), y, (unsigned)((n + y - 1) / y));
     };
+    if (p.run > 1) slots = (p.key_tiles + p.run - 1) / p.run;
     if (slots > 32768ll * 65535) return SWAA_ERR_UNSUPPORTED;
     const int rc = launch_overlapped(key_weights_kernel<D>, grid(slots), kKeyWeightsThreads, L::kBytes, st, tq, tk, p);
     if (rc != SWAA_OK || (p.chunks == 1 && p.sink_tiles == 0)) return rc;
@@ -472,8 +473,10 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < pl.bytes) return SWAA_ERR_WORKSPACE;
     DeviceInfo info;
     if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
+    const int G = Hq / Hkv, rows = last > 0 && last < max_q ? last : max_q;
+    const int hs = G % 2 == 0 && 2 * rows <= kKeyWeightsRows ? 2 : 1;
     CUtensorMap tq = {}, tk = {};
-    if (Tq > 0 && (rc = make_token_major_map(&tq, q, Tq, Hq, D, kKeyWeightsRows)) != SWAA_OK) return rc;
+    if (Tq > 0 && (rc = make_token_major_map(&tq, q, Tq, Hq, D, kKeyWeightsRows / hs, hs)) != SWAA_OK) return rc;
     if (Tk > 0) {
         rc = cu_k != nullptr ? make_token_major_map(&tk, k, Tk, Hkv, D, kKeyWeightsKeys)
                              : make_cache_map(&tk, k, paged.num_pages, paged.page_size, Hkv, D, kKeyWeightsKeys);
@@ -498,7 +501,7 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     p.weights_rows = weights_rows;
     p.Hq = Hq;
     p.Hkv = Hkv;
-    p.G = Hq / Hkv;
+    p.G = G;
     p.window = window;
     p.n_sink = n_sink;
     p.is_full = is_full ? 1 : 0;
@@ -508,6 +511,11 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     p.chunks = pl.chunks;
     p.sink_tiles = pl.sink_tiles;
     p.sink_chunks = pl.sink_chunks;
+    p.heads_per_step = hs;
+    // A block of few steps is mostly set-up: it takes more key tiles while there are several blocks per SM all the same.
+    const long long steps = std::max(1ll, ((long long)rows + kKeyWeightsRows - 1) / kKeyWeightsRows) * (G / hs);
+    p.run = 1;
+    while (p.run * steps < kKeyWeightsRunSteps && (long long)B * Hkv * (pl.key_tiles / (2 * p.run)) >= 8ll * info.sm_count) p.run *= 2;
     p.part = static_cast<float*>(workspace);
     p.sink_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_sink);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

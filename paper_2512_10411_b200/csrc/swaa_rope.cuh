@@ -197,8 +197,13 @@ __device__ __forceinline__ RopeToken rope_token(const RopeParams& p, int t, int 
     return r;
 }
 
+// Asks for a warp's share of a token ahead of its use, one 128-byte line per lane.
+__device__ __forceinline__ void rope_prefetch(const __nv_bfloat16* share, int channels, int lane) {
+    if (64 * lane < channels) asm volatile("prefetch.global.L2 [%0];" ::"l"(share + 64 * lane));
+}
+
 template <int D, bool kPairs, bool kCache>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
     using L = RopeLane<D, kPairs>;
     grid_wait();
     const int lane = threadIdx.x & 31;
@@ -217,7 +222,9 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
     float wa[8], wb[8];
     load_weights(w, ln.a0, wa);
     load_weights(w, ln.b0, wb);
+    const int share = min(heads - h0, L::kHeads * kRopeRows) * D;
     for (int t = stream; t < p.T; t += streams) {
+        if (t < p.T - streams) rope_prefetch(in + (t + streams) * stride + (long long)h0 * D, share, lane);
         uint4 xa[kRopeRows], xb[kRopeRows];
 #pragma unroll
         for (int u = 0; u < kRopeRows; ++u) {
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
 }
 
 template <int D, bool kPairs>
-__global__ void __launch_bounds__(kRopeThreads) rope_backward_kernel(const RopeGradParams p) {
+__global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const RopeGradParams p) {
     using L = RopeLane<D, kPairs>;
     __shared__ float sm_w[kRopeWarps][D];
     grid_wait();
@@ -299,7 +306,12 @@ __global__ void __launch_bounds__(kRopeThreads) rope_backward_kernel(const RopeG
     load_weights(w, ln.b0, wb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) da[i] = db[i] = 0.f;
+    const int share = min(heads - h0, L::kHeads * kRopeBwdRows) * D;
     for (int t = stream; t < p.T && stream < streams; t += streams) {
+        if (t < p.T - streams) {
+            rope_prefetch(dy_in + ((long long)(t + streams) * heads + h0) * D, share, lane);
+            if (norm) rope_prefetch(x_in + (t + streams) * x_stride + (long long)h0 * D, share, lane);
+        }
         uint4 ya[kRopeBwdRows], yb[kRopeBwdRows], xa[kRopeBwdRows], xb[kRopeBwdRows];
 #pragma unroll
         for (int u = 0; u < kRopeBwdRows; ++u) {

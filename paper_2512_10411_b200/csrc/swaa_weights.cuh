@@ -8,12 +8,13 @@
 //
 // Prompt.  With the log-sum-exp rows of the attention (lse of the prefill calls),
 //     weights_out[b, g, j] = weights_in[b, g, j] + sum over the queries i and heads h of g that see j of exp(scale q_ih . k_j - lse_ih)
-// One block owns 128 keys of one (sequence, kv head) and walks the 64-query tiles that see them, for every head of the group:
-//     S^T = K Q^T [128 keys x 64 queries], tcgen05.mma, accumulators in tensor memory
+// One block owns 128 keys of one (sequence, kv head) and walks the 128-query tiles that see them, for every head of the group:
+//     S^T = K Q^T [128 keys x 128 queries], tcgen05.mma, accumulators in tensor memory
 // so that a key is a tensor-memory lane and the sum over queries stays in its thread.  Two groups of four warps take the steps in
-// turn, four of them in flight; the log-sum-exps of a step's rows come with its queries (cp.async).  A tile seen by more than kKeyWeightsChunk
-// query tiles is cut into chunks for blocks of their own (every tile under full attention, the sinks under a window); the chunks'
-// sums are added in order by a second kernel, so results do not depend on scheduling.
+// turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than kKeyWeightsChunk query tiles is cut into
+// chunks for blocks of their own (every tile under full attention, the sinks under a window); the chunks' sums are added in order by
+// a second kernel, so results do not depend on scheduling.  Where few queries count (the last ones of a prompt) a step takes 64 queries
+// of two heads, and a block several tiles of keys one after another, its queries staying where they are.
 //
 // What bounds it: the exponentials, one per visible pair: 64 x 128 of them take 512 cycles of an SM's special-function units, the
 // products of a step at D = 128 256 cycles of its tensor cores.
@@ -86,14 +87,17 @@ struct KeyWeightsParams {
     float sl2;
     // chunks: [chunks][B][Hkv][128 key_tiles] sums of all tiles, [sink_chunks][B][Hkv][128 sink_tiles] of the tiles that hold sinks
     int key_tiles, chunks, sink_tiles, sink_chunks;
+    int run;                      // key tiles of a block, one after another; above 1 nothing is cut into chunks
+    int heads_per_step;           // 2: a step takes 64 queries of two heads (at most 64 queries of a sequence count)
     float *part, *sink_part;
 };
 
 constexpr int kKeyWeightsKeys = 128;
-constexpr int kKeyWeightsRows = 64;    // queries of a step
-constexpr int kKeyWeightsChunk = 32;   // query tiles of a block
+constexpr int kKeyWeightsRows = 128;   // columns of a step: queries, or queries of two heads in turn
+constexpr int kKeyWeightsChunk = 16;   // query tiles of a block
 constexpr int kKeyWeightsThreads = 320;  // two groups of four warps, producer, issuer
-constexpr int kKeyWeightsBuffers = 4;  // S^T in tensor memory; half of it per block, two blocks per SM
+constexpr int kKeyWeightsRunSteps = 16;  // steps below which a block takes more key tiles
+constexpr int kKeyWeightsLse = 4;      // steps whose log-sum-exps are in shared memory
 
 // One sequence of a call, checked against what the call says of it.
 struct KeyWeightsSeq {
@@ -115,7 +119,7 @@ __device__ __forceinline__ KeyWeightsSeq key_weights_seq(const KeyWeightsParams&
     s.pos0 = s.len_k - s.nq;
     return s;
 }
-// Query tiles [lo, hi] (64 rows from pos0 on) that see a key of the tile at j0, and their chunks; none: hi < lo, 0 chunks.
+// Query tiles [lo, hi] (128 rows from pos0 on) that see a key of the tile at j0, and their chunks; none: hi < lo, 0 chunks.
 struct KeyWeightsSpan {
     int lo, hi, chunks;
 };
@@ -143,14 +147,14 @@ __device__ __forceinline__ float key_weights_old(const KeyWeightsParams& p, cons
 template <int D>
 struct KeyWeightsSmem {
     static constexpr int kPanels = D / 64;
-    static constexpr int kStages = D == 128 ? 4 : 8;  // two blocks per SM at either size
-    static constexpr int kKPanelBytes = kKeyWeightsKeys * 128, kKBytes = kPanels * kKPanelBytes;
-    static constexpr int kQPanelBytes = kKeyWeightsRows * 128, kQBytes = kPanels * kQPanelBytes;
-    static constexpr int kOffRing = kKBytes;
-    static constexpr int kOffLse = kOffRing + kStages * kQBytes;
-    static constexpr int kOffSum = kOffLse + kStages * kKeyWeightsRows * 4;
+    static constexpr int kStages = D == 128 ? 2 : 4;  // two blocks per SM at either size
+    static constexpr int kPanelBytes = 128 * 128;     // 128 rows of 64 channels
+    static constexpr int kTileBytes = kPanels * kPanelBytes;
+    static constexpr int kOffRing = kTileBytes;       // K first
+    static constexpr int kOffLse = kOffRing + kStages * kTileBytes;
+    static constexpr int kOffSum = kOffLse + kKeyWeightsLse * kKeyWeightsRows * 4;
     static constexpr int kOffBar = kOffSum + kKeyWeightsKeys * 4;
-    static constexpr int kNumBars = 1 + 2 * kStages + 2 * kKeyWeightsBuffers + 1;
+    static constexpr int kNumBars = 2 + 2 * kStages + 2 * kKeyWeightsLse + 4 + 1;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two blocks per SM");
@@ -165,11 +169,17 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
+// Keeps the uses of 32 registers that an asynchronous tensor-memory load fills behind the wait for it.
+__device__ __forceinline__ void pin32(uint32_t* r) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+}
+
 template <int D>
 __global__ void __launch_bounds__(kKeyWeightsThreads, 2)
 key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const KeyWeightsParams p) {
     using L = KeyWeightsSmem<D>;
-    constexpr int BK = kKeyWeightsKeys, BR = kKeyWeightsRows, NQ = L::kStages, NB = kKeyWeightsBuffers;
+    constexpr int BK = kKeyWeightsKeys, BR = kKeyWeightsRows, NQ = L::kStages, NL = kKeyWeightsLse;
     constexpr uint32_t kIdS = make_idesc(BK, BR, 0);
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     const uint32_t smem_base = smem_u32(smem_raw);
@@ -181,7 +191,8 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     float* s_sum = reinterpret_cast<float*>(smem_raw + L::kOffSum);
     const uint32_t sK = smem_base, sRing = smem_base + L::kOffRing, bars = smem_base + L::kOffBar;
     auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
-    constexpr int BAR_K = 0, BAR_QF = 1, BAR_QE = BAR_QF + NQ, BAR_SF = BAR_QE + NQ, BAR_SE = BAR_SF + NB, BAR_FIN = BAR_SE + NB;
+    constexpr int BAR_KF = 0, BAR_KE = 1, BAR_QF = 2, BAR_QE = BAR_QF + NQ, BAR_LF = BAR_QE + NQ, BAR_LE = BAR_LF + NL, BAR_SF = BAR_LE + NL;
+    constexpr int BAR_SE = BAR_SF + 2, BAR_FIN = BAR_SE + 2;
     static_assert(BAR_FIN + 1 == L::kNumBars, "barrier count");
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem_raw + L::kOffMisc);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -190,49 +201,71 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int b = (int)blockIdx.x / p.Hkv, hk = (int)blockIdx.x - b * p.Hkv;
     // blocks start in the order of their index, x first: the tiles that hold sinks, then all tiles from the first key on
-    int slot = (int)(blockIdx.z * gridDim.y + blockIdx.y), tile, chunk;
+    int slot = (int)(blockIdx.z * gridDim.y + blockIdx.y), tile0, chunk;
     const bool sinks = slot < p.sink_tiles * p.sink_chunks;
     if (sinks) {
-        tile = slot / p.sink_chunks;
-        chunk = slot - tile * p.sink_chunks;
+        tile0 = slot / p.sink_chunks;
+        chunk = slot - tile0 * p.sink_chunks;
     } else {
         slot -= p.sink_tiles * p.sink_chunks;
-        tile = slot / p.chunks;
-        chunk = slot - tile * p.chunks;
-        if (tile < p.sink_tiles || tile >= p.key_tiles) return;
+        tile0 = slot / p.chunks;
+        chunk = slot - tile0 * p.chunks;
+        tile0 *= p.run;
+        if (tile0 < p.sink_tiles || tile0 >= p.key_tiles) return;
     }
     const KeyWeightsSeq s = key_weights_seq(p, b);
-    const int j0 = tile * BK;
     if (!s.ok) {
         if (threadIdx.x == 0 && chunk == 0) record_device_error(SWAA_ERR_BAD_SEQLENS);
         return;
     }
-    if (j0 >= s.len_k) return;
-    const KeyWeightsSpan span = key_weights_span(p, s, j0);
+    if (tile0 * BK >= s.len_k) return;
+    const int tile1 = min(tile0 + (sinks ? 1 : p.run), (s.len_k + BK - 1) / BK);
     const size_t row = (size_t)b * p.Hkv + hk;
-    if (span.chunks == 0) {  // no query of the call sees the tile
-        const int j = j0 + (int)threadIdx.x;
-        if (chunk == 0 && (int)threadIdx.x < BK && j < s.len_k) p.weights_out[row * p.weights_rows + j] = key_weights_old(p, s, row, j);
+
+    // One tile of the run: the query tiles m_lo .. m_lo + nm - 1 that this block takes, for every group of heads_per_step heads.
+    const int hs = p.heads_per_step, shift = hs - 1, head_steps = p.G / hs;
+    struct Tile {
+        int m_lo, nm, page;
+        KeyWeightsSpan span;
+    };
+    auto tile_of = [&](int t) {
+        Tile x;
+        x.span = key_weights_span(p, s, t * BK);
+        x.m_lo = x.nm = x.page = 0;
+        if (chunk < x.span.chunks) {  // an even share of the span
+            const int n = x.span.hi - x.span.lo + 1, share = (n + x.span.chunks - 1) / x.span.chunks;
+            x.m_lo = x.span.lo + chunk * share;
+            x.nm = max(min(x.span.hi, x.m_lo + share - 1) - x.m_lo + 1, 0);
+        }
+        if (p.cu_k == nullptr && (x.page = key_weights_page(p, b, t * BK)) < 0) x.nm = 0;
+        return x;
+    };
+    // What the block found out for key j of tile t: the whole sum, or that of its chunk.
+    auto store = [&](const Tile& x, int j, float total) {
+        if (j >= s.len_k) return;
+        if (x.page < 0) {
+            record_device_error(SWAA_ERR_BAD_SEQLENS);
+        } else if (x.span.chunks <= 1) {
+            if (chunk == 0) p.weights_out[row * p.weights_rows + j] = key_weights_old(p, s, row, j) + total;
+        } else if (chunk < x.span.chunks) {
+            if (sinks) p.sink_part[((size_t)chunk * p.B * p.Hkv + row) * (p.sink_tiles * BK) + j] = total;
+            else p.part[((size_t)chunk * p.B * p.Hkv + row) * ((size_t)p.key_tiles * BK) + j] = total;
+        }
+    };
+    bool any = false;  // uniform
+    for (int t = tile0; t < tile1; ++t) any = any || tile_of(t).nm > 0;
+    if (!any) {  // no query of the block sees a key of it
+        for (int t = tile0; t < tile1; ++t)
+            if ((int)threadIdx.x < BK) store(tile_of(t), t * BK + (int)threadIdx.x, 0.f);
         return;
     }
-    if (chunk >= span.chunks) return;
-    int page = 0;
-    if (p.cu_k == nullptr && (page = key_weights_page(p, b, j0)) < 0) {
-        if (threadIdx.x == 0) record_device_error(SWAA_ERR_BAD_SEQLENS);
-        return;
-    }
-    // an even share of the span's tiles
-    const int span_tiles = span.hi - span.lo + 1, share = (span_tiles + span.chunks - 1) / span.chunks;
-    const int m_lo = span.lo + chunk * share, m_hi = min(span.hi, m_lo + share - 1);
-    const int nm = max(m_hi - m_lo + 1, 0), n_steps = nm * p.G;
 
     if (threadIdx.x == 0) {
         *abort_flag = 0;
         for (int i = 0; i < L::kNumBars; ++i) {
             uint32_t count = 1u;
-            if (i >= BAR_QF && i < BAR_QF + NQ) count = 33u;  // the copy of the queries, and 32 lanes with the log-sum-exps
-            if (i >= BAR_QE && i < BAR_QE + NQ) count = 5u;   // the products, and four warps that have read the log-sum-exps
-            if (i >= BAR_SE && i < BAR_SE + NB) count = 4u;   // four warps that have read S^T
+            if (i >= BAR_LF && i < BAR_LF + NL) count = 32u;  // the lanes that copy
+            if ((i >= BAR_LE && i < BAR_LE + NL) || (i >= BAR_SE && i < BAR_SE + 2)) count = 4u;  // the warps of a group
             mbar_init(bar(i), count);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -245,54 +278,64 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    static_assert(NB * BR == 256, "tensor memory columns");
+    static_assert(2 * BR == 256, "tensor memory columns");
+    // Where every tile of the run meets the same few queries, they are loaded once and stay.
+    const bool resident = p.run > 1 && s.nq <= BR / hs && head_steps <= NQ;
     bool ok = true;
-    float total = 0.f;
 
     if (warp == 8) {
         // ================================================================================= producer
-        if (lane == 0) {
-            mbar_arrive_expect_tx(bar(BAR_K), (uint32_t)L::kKBytes);
-#pragma unroll
-            for (int pn = 0; pn < L::kPanels; ++pn) {
-                if (p.cu_k != nullptr) tma_load_3d(sK + pn * L::kKPanelBytes, &tm_k, pn * 64, hk, s.k0 + j0, bar(BAR_K));
-                else tma_load_4d(sK + pn * L::kKPanelBytes, &tm_k, pn * 64, hk, j0 % p.page_size, page, bar(BAR_K));
-            }
-        }
         const int first = s.q0 + s.len_q - s.nq;  // packed row of the query at pos0
-        int issued = 0;
-        for (int st = 0, n = 0, h = 0, m = 0; n < n_steps; ++n) {
-            if (n >= NQ) ok = mbar_wait(bar(BAR_QE + st), (uint32_t)(n / NQ - 1) & 1u, abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
+        int tiles = 0, loads = 0, steps = 0;      // so far
+        for (int t = tile0; t < tile1 && ok; ++t) {
+            const Tile x = tile_of(t);
+            if (x.nm == 0) continue;
+            if (tiles > 0) ok = warp_wait(bar(BAR_KE), (uint32_t)(tiles - 1) & 1u, abort_flag);
             if (!ok) break;
-            const int head = hk * p.G + h, i0 = (m_lo + m) * BR;  // from pos0
+            ++tiles;
             if (lane == 0) {
-                mbar_arrive_expect_tx(bar(BAR_QF + st), (uint32_t)L::kQBytes);
+                mbar_arrive_expect_tx(bar(BAR_KF), (uint32_t)L::kTileBytes);
 #pragma unroll
-                for (int pn = 0; pn < L::kPanels; ++pn)
-                    tma_load_3d(sRing + (uint32_t)(st * L::kQBytes + pn * L::kQPanelBytes), &tm_q, pn * 64, head, first + i0, bar(BAR_QF + st));
+                for (int pn = 0; pn < L::kPanels; ++pn) {
+                    if (p.cu_k != nullptr) tma_load_3d(sK + pn * L::kPanelBytes, &tm_k, pn * 64, hk, s.k0 + t * BK, bar(BAR_KF));
+                    else tma_load_4d(sK + pn * L::kPanelBytes, &tm_k, pn * 64, hk, t * BK % p.page_size, x.page, bar(BAR_KF));
+                }
             }
+            for (int h = 0; h < head_steps && ok; ++h)
+                for (int m = 0; m < x.nm; ++m) {
+                    const int head = hk * p.G + h * hs, i0 = (x.m_lo + m) * BR;  // from pos0
+                    if (!resident || tiles == 1) {
+                        const int st = loads % NQ;
+                        if (loads >= NQ) ok = warp_wait(bar(BAR_QE + st), (uint32_t)(loads / NQ - 1) & 1u, abort_flag);
+                        if (!ok) break;
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(bar(BAR_QF + st), (uint32_t)L::kTileBytes);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int r = lane + 32 * e;
-                const bool on = i0 + r < s.nq;
-                cp_async_4(smem_u32(s_lse + st * BR + r), p.lse + (size_t)head * p.Tq + first + (on ? i0 + r : 0), on);
-            }
-            cp_async_arrive(bar(BAR_QF + st));
-            issued = n + 1;
-            if (++m == nm) {
-                m = 0;
-                ++h;
-            }
-            if (++st == NQ) st = 0;
+                            for (int pn = 0; pn < L::kPanels; ++pn)
+                                tma_load_3d(sRing + (uint32_t)(st * L::kTileBytes + pn * L::kPanelBytes), &tm_q, pn * 64, head, first + i0, bar(BAR_QF + st));
+                        }
+                        ++loads;
+                    }
+                    const int sl = steps % NL;
+                    if (steps >= NL) ok = warp_wait(bar(BAR_LE + sl), (uint32_t)(steps / NL - 1) & 1u, abort_flag);
+                    if (!ok) break;
+#pragma unroll
+                    for (int e = 0; e < BR / 32; ++e) {
+                        const int c = lane + 32 * e, r = i0 + (c >> shift);
+                        const bool on = r < s.nq;
+                        cp_async_4(smem_u32(s_lse + sl * BR + c), p.lse + (size_t)(head + (c & shift)) * p.Tq + first + (on ? r : 0), on);
+                    }
+                    cp_async_arrive(bar(BAR_LF + sl));
+                    ++steps;
+                }
         }
         if (!ok) {  // give outstanding copies a bounded chance to land before the block's memory is released
             asm volatile("cp.async.wait_all;" ::: "memory");
             const uint64_t t0 = global_timer_ns();
             bool landed = false;
             while (!landed && global_timer_ns() - t0 < kWaitLimitNs) {
-                landed = mbar_try_wait(bar(BAR_K), 0u);
-                for (int n = max(0, issued - NQ); n < issued; ++n) landed = landed && mbar_try_wait(bar(BAR_QF + n % NQ), (uint32_t)(n / NQ) & 1u);
+                landed = tiles == 0 || mbar_try_wait(bar(BAR_KF), (uint32_t)(tiles - 1) & 1u);
+                for (int n = max(0, loads - NQ); n < loads; ++n) landed = landed && mbar_try_wait(bar(BAR_QF + n % NQ), (uint32_t)(n / NQ) & 1u);
             }
         }
         __syncwarp();
@@ -301,31 +344,30 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const bool el = elect_one();
         const uint32_t hi = (uint32_t)(smem_desc_sw128(0, 0, 1024) >> 32);
         const uint32_t k_a = (uint32_t)smem_desc_sw128(sK, 16, 1024), q_b = (uint32_t)smem_desc_sw128(sRing, 16, 1024);
-        ok = warp_wait(bar(BAR_K), 0u, abort_flag);
-        int st = 0, buf = 0;
-        uint32_t st_ph = 0, buf_ph = 1;  // the buffers start out free
-        for (int n = 0; n < n_steps && ok; ++n) {
-            ok = warp_wait(bar(BAR_QF + st), st_ph, abort_flag) && warp_wait(bar(BAR_SE + buf), buf_ph, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            if (el) {
-                const uint32_t d = tmem_base + (uint32_t)(BR * buf), q = q_b + (((uint32_t)st * L::kQBytes) >> 4);
+        int tiles = 0, n = 0;  // n: steps so far
+        for (int t = tile0; t < tile1 && ok; ++t) {
+            const Tile x = tile_of(t);
+            const int n_steps = x.nm * head_steps;
+            if (n_steps == 0) continue;
+            ok = warp_wait(bar(BAR_KF), (uint32_t)tiles & 1u, abort_flag);
+            ++tiles;
+            for (int i = 0; i < n_steps && ok; ++i, ++n) {
+                const int ld = resident ? i : n, st = ld % NQ, buf = n & 1;
+                ok = warp_wait(bar(BAR_QF + st), (uint32_t)(ld / NQ) & 1u, abort_flag) &&
+                     warp_wait(bar(BAR_SE + buf), ((uint32_t)(n >> 1) & 1u) ^ 1u, abort_flag);  // the buffers start out free
+                if (!ok) break;
+                tc_fence_after();
+                if (el) {
+                    const uint32_t d = tmem_base + (uint32_t)(BR * buf), q = q_b + (((uint32_t)st * L::kTileBytes) >> 4);
 #pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    const uint32_t oa = ((uint32_t)(kk >> 2) * L::kKPanelBytes + (uint32_t)(kk & 3) * 32u) >> 4;
-                    const uint32_t ob = ((uint32_t)(kk >> 2) * L::kQPanelBytes + (uint32_t)(kk & 3) * 32u) >> 4;
-                    mma_ss_lh(d, k_a + oa, q + ob, hi, kIdS, kk > 0 ? 1u : 0u);
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        const uint32_t o = ((uint32_t)(kk >> 2) * L::kPanelBytes + (uint32_t)(kk & 3) * 32u) >> 4;
+                        mma_ss_lh(d, k_a + o, q + o, hi, kIdS, kk > 0 ? 1u : 0u);
+                    }
+                    tc_commit(bar(BAR_SF + buf));
+                    if (!resident) tc_commit(bar(BAR_QE + st));
+                    if (i == n_steps - 1) tc_commit(bar(BAR_KE));
                 }
-                tc_commit(bar(BAR_SF + buf));
-                tc_commit(bar(BAR_QE + st));
-            }
-            if (++st == NQ) {
-                st = 0;
-                st_ph ^= 1u;
-            }
-            if (++buf == NB) {
-                buf = 0;
-                buf_ph ^= 1u;
             }
         }
         // all products issued by this warp must have retired before the tensor memory is freed
@@ -334,65 +376,93 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         __syncwarp();
     } else {
         // =============================================================================== exponentials
+        // Group n & 1 takes step n of the block; the groups' sums of a tile meet in the warps of the first.
         const int grp = warp >> 2, quad = warp & 3, kl = 32 * quad + lane;
-        const int j = j0 + kl;
         const bool full = p.is_full != 0;
-        const int vis_hi = (full || j < p.n_sink) ? s.len_k : (int)min((long long)s.len_k, (long long)j + p.window);
+        const uint32_t tS = tmem_base + ((uint32_t)(32 * quad) << 16) + (uint32_t)(BR * grp);
         const uint64_t sl2x2 = pack_f32x2(p.sl2, p.sl2), nlog2e = pack_f32x2(-1.4426950408889634f, -1.4426950408889634f);
-        for (int n = grp; n < n_steps; n += 2) {
-            const int st = n % NQ, buf = n % NB, i0 = s.pos0 + (m_lo + n % nm) * BR;  // position of the tile's first query
-            ok = warp_wait(bar(BAR_QF + st), (uint32_t)(n / NQ) & 1u, abort_flag) && warp_wait(bar(BAR_SF + buf), (uint32_t)(n / NB) & 1u, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            const bool need_mask = i0 + BR > s.len_k || tile_needs_mask(i0, i0 + BR - 1, j0, j0 + BK - 1, p.window, p.n_sink, full);
-            uint64_t sum[2] = {0ull, 0ull};
-            auto half = [&](auto mask_tag, int c0) {
-                constexpr bool kMask = decltype(mask_tag)::value;
-                uint32_t sv[32];
-                tmem_ld32(tmem_base + ((uint32_t)(32 * quad) << 16) + (uint32_t)(BR * buf + c0), sv);
-                tc_wait_ld();
-                const float* lse = s_lse + st * BR + c0;
-                const int r_lo = j - i0 - c0, r_hi = vis_hi - i0 - c0;  // visible queries of this half
+        int base = 0;  // steps of the tiles before
+        for (int t = tile0; t < tile1; ++t) {
+            const Tile x = tile_of(t);
+            const int j0 = t * BK, jw = j0 + 32 * quad, j = j0 + kl, n_steps = x.nm * head_steps;
+            const int vis_hi = (full || j < p.n_sink) ? s.len_k : (int)min((long long)s.len_k, (long long)j + p.window);
+            float total = 0.f;
+            int m = (base ^ grp) & 1;  // first step of this group, then every other one
+            for (int i = m; i < n_steps && ok; i += 2) {
+                const int n = base + i, sl = n % NL;
+                while (m >= x.nm) m -= x.nm;
+                const int i0 = s.pos0 + (x.m_lo + m) * BR;  // position of the first query
+                m += 2;
+                ok = warp_wait(bar(BAR_LF + sl), (uint32_t)(n / NL) & 1u, abort_flag) && warp_wait(bar(BAR_SF + grp), (uint32_t)(n >> 1) & 1u, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                const int i1 = i0 + ((BR - 1) >> shift);
+                const bool edge = i1 >= s.len_k || tile_needs_mask(i0, i1, j0, j0 + BK - 1, p.window, p.n_sink, full);
+                uint64_t sum[2] = {0ull, 0ull};
+                const float* lse = s_lse + sl * BR;
+                // 32 columns from c0 on, whose scores are in sv
+                auto columns = [&](auto mask_tag, int c0, const uint32_t* sv) {
+                    constexpr bool kMask = decltype(mask_tag)::value;
+                    const int r_lo = min(max(j - i0, 0), BR) * hs - c0, r_hi = min(max(vis_hi - i0, 0), BR) * hs - c0;  // visible ones
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 l4 = *reinterpret_cast<const float4*>(lse + e);
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 l4 = *reinterpret_cast<const float4*>(lse + c0 + e);
 #pragma unroll
-                    for (int u = 0; u < 4; u += 2) {
-                        uint64_t c;
-                        asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(u ? pack_f32x2(l4.z, l4.w) : pack_f32x2(l4.x, l4.y)), "l"(nlog2e));
-                        const uint64_t x = fma_f32x2(pack_f32x2(__uint_as_float(sv[e + u]), __uint_as_float(sv[e + u + 1])), sl2x2, c);
-                        float x0, x1;
-                        unpack_f32x2(x, x0, x1);
-                        x0 = ex2f(x0);
-                        x1 = ex2f(x1);
-                        if (kMask) {
-                            x0 = e + u >= r_lo && e + u < r_hi ? x0 : 0.f;
-                            x1 = e + u + 1 >= r_lo && e + u + 1 < r_hi ? x1 : 0.f;
+                        for (int u = 0; u < 4; u += 2) {
+                            uint64_t c;
+                            asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c) : "l"(u ? pack_f32x2(l4.z, l4.w) : pack_f32x2(l4.x, l4.y)), "l"(nlog2e));
+                            const uint64_t v = fma_f32x2(pack_f32x2(__uint_as_float(sv[e + u]), __uint_as_float(sv[e + u + 1])), sl2x2, c);
+                            float x0, x1;
+                            unpack_f32x2(v, x0, x1);
+                            x0 = ex2f(x0);
+                            x1 = ex2f(x1);
+                            if (kMask) {
+                                x0 = e + u >= r_lo && e + u < r_hi ? x0 : 0.f;
+                                x1 = e + u + 1 >= r_lo && e + u + 1 < r_hi ? x1 : 0.f;
+                            }
+                            sum[u >> 1] = add_f32x2(sum[u >> 1], pack_f32x2(x0, x1));
                         }
-                        sum[u >> 1] = add_f32x2(sum[u >> 1], pack_f32x2(x0, x1));
                     }
+                };
+                auto release = [&] {  // the products of the group's next step may overwrite the scores
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(BAR_SE + grp));
+                    __syncwarp();
+                };
+#pragma unroll 1
+                for (int c0 = 0; c0 < BR; c0 += 32) {
+                    const int ia = i0 + (c0 >> shift), ib = i0 + ((c0 + 31) >> shift);
+                    // the warp's 32 keys and these queries: nothing visible, nothing hidden, or both
+                    const bool none = edge && (ib < jw || ia >= s.len_k || !(full || jw < p.n_sink || (long long)ia < (long long)jw + 31 + p.window));
+                    uint32_t sv[32];
+                    if (!none) {
+                        tmem_ld32(tS + (uint32_t)c0, sv);
+                        tc_wait_ld();
+                        pin32(sv);
+                    }
+                    if (c0 == BR - 32) release();
+                    if (none) continue;
+                    if (!edge || (ib < s.len_k && !tile_needs_mask(ia, ib, jw, jw + 31, p.window, p.n_sink, full))) columns(std::false_type{}, c0, sv);
+                    else columns(std::true_type{}, c0, sv);
                 }
-            };
-            if (need_mask) {
-                half(std::true_type{}, 0);
-                half(std::true_type{}, 32);
-            } else {
-                half(std::false_type{}, 0);
-                half(std::false_type{}, 32);
+                float a, c, d, e;
+                unpack_f32x2(sum[0], a, c);
+                unpack_f32x2(sum[1], d, e);
+                total += (a + c) + (d + e);  // a step's terms at a time, so that long sums keep their bits
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_LE + sl));
+                __syncwarp();
             }
-            float a, c, d, e;
-            unpack_f32x2(sum[0], a, c);
-            unpack_f32x2(sum[1], d, e);
-            total += (a + c) + (d + e);  // 64 terms at a time, so that long sums keep their bits
-            tc_fence_before();
+            base += n_steps;
+            // the two warps that hold the same keys meet here, whatever their waits gave
+            if (grp == 1) s_sum[kl] = total;
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(bar(BAR_SE + buf));
-                mbar_arrive(bar(BAR_QE + st));
-            }
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
+            if (grp == 0 && *abort_flag == 0) store(x, j, total + s_sum[kl]);
             __syncwarp();
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
         }
-        if (grp == 1) s_sum[kl] = total;
     }
 
     // ---- every thread arrives here (also after a failed wait)
@@ -401,14 +471,6 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (warp == 9) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256u) : "memory");
-    } else if (warp < 4 && *abort_flag == 0) {
-        const int kl = (int)threadIdx.x, j = j0 + kl;
-        if (j < s.len_k) {
-            total += s_sum[kl];
-            if (span.chunks == 1) p.weights_out[row * p.weights_rows + j] = key_weights_old(p, s, row, j) + total;
-            else if (sinks) p.sink_part[((size_t)chunk * p.B * p.Hkv + row) * (p.sink_tiles * BK) + j] = total;
-            else p.part[((size_t)chunk * p.B * p.Hkv + row) * ((size_t)p.key_tiles * BK) + j] = total;
-        }
     }
 }
 
