@@ -153,7 +153,7 @@ struct KeyWeightsSmem {
     static constexpr int kOffRing = kTileBytes;       // K first
     static constexpr int kOffLse = kOffRing + kStages * kTileBytes;
     static constexpr int kOffSum = kOffLse + kKeyWeightsLse * kKeyWeightsRows * 4;
-    static constexpr int kOffBar = kOffSum + kKeyWeightsKeys * 4;
+    static constexpr int kOffBar = kOffSum + 2 * kKeyWeightsKeys * 4;
     static constexpr int kNumBars = 2 + 2 * kStages + 2 * kKeyWeightsLse + 4 + 1;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
@@ -169,10 +169,10 @@ __device__ __forceinline__ void cp_async_arrive(uint32_t bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 
-// Keeps the uses of 32 registers that an asynchronous tensor-memory load fills behind the wait for it.
-__device__ __forceinline__ void pin32(uint32_t* r) {
+// Keeps the uses of 16 registers that an asynchronous tensor-memory load fills behind the wait for it.
+__device__ __forceinline__ void pin16(uint32_t* r) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[i]));
+    for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
 }
 
 template <int D>
@@ -232,7 +232,10 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         Tile x;
         x.span = key_weights_span(p, s, t * BK);
         x.m_lo = x.nm = x.page = 0;
-        if (chunk < x.span.chunks) {  // an even share of the span
+        if (x.span.chunks == 1 && chunk == 0) {
+            x.m_lo = x.span.lo;
+            x.nm = x.span.hi - x.span.lo + 1;
+        } else if (chunk < x.span.chunks) {  // an even share of the span
             const int n = x.span.hi - x.span.lo + 1, share = (n + x.span.chunks - 1) / x.span.chunks;
             x.m_lo = x.span.lo + chunk * share;
             x.nm = max(min(x.span.hi, x.m_lo + share - 1) - x.m_lo + 1, 0);
@@ -401,11 +404,12 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 uint64_t sum[2] = {0ull, 0ull};
                 const float* lse = s_lse + sl * BR;
                 // 32 columns from c0 on, whose scores are in sv
-                auto columns = [&](auto mask_tag, int c0, const uint32_t* sv) {
+                auto columns = [&](auto mask_tag, auto count_tag, int c0, const uint32_t* sv) {
                     constexpr bool kMask = decltype(mask_tag)::value;
+                    constexpr int kCount = decltype(count_tag)::value;
                     const int r_lo = min(max(j - i0, 0), BR) * hs - c0, r_hi = min(max(vis_hi - i0, 0), BR) * hs - c0;  // visible ones
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
+                    for (int e = 0; e < kCount; e += 4) {
                         const float4 l4 = *reinterpret_cast<const float4*>(lse + c0 + e);
 #pragma unroll
                         for (int u = 0; u < 4; u += 2) {
@@ -430,21 +434,40 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                     if (lane == 0) mbar_arrive(bar(BAR_SE + grp));
                     __syncwarp();
                 };
+                if (!edge) {  // the next columns on their way while the exponentials of these are taken
+                    using N = std::integral_constant<int, 16>;
+                    uint32_t sa[16], sb[16];
+                    tmem_ld16(tS, sa);
+                    tc_wait_ld();
+                    pin16(sa);
+#pragma unroll
+                    for (int c0 = 0; c0 < BR; c0 += 32) {
+                        tmem_ld16(tS + (uint32_t)(c0 + 16), sb);
+                        columns(std::false_type{}, N{}, c0, sa);
+                        tc_wait_ld();
+                        pin16(sb);
+                        if (c0 + 32 < BR) tmem_ld16(tS + (uint32_t)(c0 + 32), sa);
+                        else release();
+                        columns(std::false_type{}, N{}, c0 + 16, sb);
+                        if (c0 + 32 < BR) {
+                            tc_wait_ld();
+                            pin16(sa);
+                        }
+                    }
+                } else {
+                    using N = std::integral_constant<int, 32>;
 #pragma unroll 1
-                for (int c0 = 0; c0 < BR; c0 += 32) {
-                    const int ia = i0 + (c0 >> shift), ib = i0 + ((c0 + 31) >> shift);
-                    // the warp's 32 keys and these queries: nothing visible, nothing hidden, or both
-                    const bool none = edge && (ib < jw || ia >= s.len_k || !(full || jw < p.n_sink || (long long)ia < (long long)jw + 31 + p.window));
-                    uint32_t sv[32];
-                    if (!none) {
+                    for (int c0 = 0; c0 < BR; c0 += 32) {
+                        const int ia = i0 + (c0 >> shift), ib = i0 + ((c0 + 31) >> shift);
+                        // the warp's 32 keys and these queries: nothing visible, nothing hidden, or both
+                        if (ib < jw || ia >= s.len_k || !(full || jw < p.n_sink || (long long)ia < (long long)jw + 31 + p.window)) continue;
+                        uint32_t sv[32];
                         tmem_ld32(tS + (uint32_t)c0, sv);
                         tc_wait_ld();
-                        pin32(sv);
+                        if (ib < s.len_k && !tile_needs_mask(ia, ib, jw, jw + 31, p.window, p.n_sink, full)) columns(std::false_type{}, N{}, c0, sv);
+                        else columns(std::true_type{}, N{}, c0, sv);
                     }
-                    if (c0 == BR - 32) release();
-                    if (none) continue;
-                    if (!edge || (ib < s.len_k && !tile_needs_mask(ia, ib, jw, jw + 31, p.window, p.n_sink, full))) columns(std::false_type{}, c0, sv);
-                    else columns(std::true_type{}, c0, sv);
+                    release();
                 }
                 float a, c, d, e;
                 unpack_f32x2(sum[0], a, c);
@@ -455,13 +478,14 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 __syncwarp();
             }
             base += n_steps;
-            // the two warps that hold the same keys meet here, whatever their waits gave
-            if (grp == 1) s_sum[kl] = total;
+            // The two warps that hold the same keys meet here, whatever their waits gave.  (The first group reads its buffer before it
+            // gets to the next meeting, the second writes it again after that one.)
+            float* meet = s_sum + (t & 1) * BK;
+            if (grp == 1) meet[kl] = total;
             __syncwarp();
             asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
-            if (grp == 0 && *abort_flag == 0) store(x, j, total + s_sum[kl]);
+            if (grp == 0 && *abort_flag == 0) store(x, j, total + meet[kl]);
             __syncwarp();
-            asm volatile("bar.sync %0, 64;" ::"r"(1 + quad) : "memory");
         }
     }
 
