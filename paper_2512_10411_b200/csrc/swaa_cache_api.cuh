@@ -20,29 +20,22 @@ static int check_rope(int T, int Hq, int Hkv, int D, int rotary_dim, const float
     return SWAA_OK;
 }
 
-// Warps' shares of one token: groups of heads of one kind.
-template <typename P>
-static void rope_segments(P* p, int Hq, int Hkv, int D, int rows, bool values) {
-    const int per = rows * (32 / (D / 16));
-    p->seg_q = (Hq + per - 1) / per;
-    p->seg_k = (Hkv + per - 1) / per;
-    p->segs = p->seg_q + p->seg_k * (values ? 2 : 1);
-}
+constexpr int kRopeBlocksPerSm = 2;
 
-// Blocks of a launch: one warp per share of a token, as many as the SMs hold at a time; the warps go on through the tokens.
-static unsigned rope_blocks(int T, int segs, int sms, int per_sm) {
-    const long long most = std::max((long long)sms * per_sm, ((long long)segs + kRopeWarps - 1) / kRopeWarps);
-    return (unsigned)std::min(((long long)T * segs + kRopeWarps - 1) / kRopeWarps, most);
+// Blocks of a launch: a warp per share of a token, as many as the SMs hold at a time; the warps go on through the tokens.
+static unsigned rope_blocks(int T, const RopeSplit& s, int sms) {
+    const long long most = std::max((long long)sms * kRopeBlocksPerSm, ((long long)s.segs + kRopeWarps - 1) / kRopeWarps);
+    return (unsigned)std::min(((long long)T * s.segs + kRopeWarps - 1) / kRopeWarps, most);
 }
-
-constexpr int kRopeBlocksPerSm = 2, kRopeBwdBlocksPerSm = 2;
 
 template <bool kCache>
 static int launch_rope(const RopeParams& p, int D, bool pairs, int sms, cudaStream_t st) {
-    const dim3 grid(rope_blocks(p.T, p.segs, sms, kRopeBlocksPerSm));
+    const dim3 grid(rope_blocks(p.T, RopeSplit(p.Hq, p.Hkv, D, kRopeRows, p.v != nullptr), sms));
     auto* kernel = D == 128 ? (pairs ? rope_kernel<128, true, kCache> : rope_kernel<128, false, kCache>)
                             : (pairs ? rope_kernel<64, true, kCache> : rope_kernel<64, false, kCache>);
-    return launch_overlapped(kernel, grid, kRopeThreads, 0, st, p);
+    static std::atomic<bool> attr_done[4][64];
+    if (ensure_dynamic_smem(kernel, kRopeSmem, attr_done[(D == 128 ? 2 : 0) + (pairs ? 1 : 0)]) != SWAA_OK) return SWAA_ERR_CUDA;
+    return launch_overlapped(kernel, grid, kRopeThreads, kRopeSmem, st, p);
 }
 
 static int current_sm100(DeviceInfo* info) {
@@ -73,7 +66,6 @@ static RopeParams rope_params(const void* q, const void* k, const void* v, long 
     p.q_out = static_cast<__nv_bfloat16*>(q_out);
     p.k_out = static_cast<__nv_bfloat16*>(k_out);
     p.v_out = static_cast<__nv_bfloat16*>(v_out);
-    rope_segments(&p, Hq, Hkv, D, kRopeRows, v != nullptr);
     return p;
 }
 
@@ -134,9 +126,8 @@ extern "C" size_t swaa_qk_norm_rope_backward_workspace_size(int T, int Hq, int H
     if (T < 1 || check_rope(T, Hq, Hkv, D, 0, nullptr, nullptr, nullptr, 0.f) != SWAA_OK) return 256;
     DeviceInfo info;
     if (current_device_info(&info) != SWAA_OK) info.sm_count = 148;
-    RopeGradParams p;
-    rope_segments(&p, Hq, Hkv, D, kRopeBwdRows, true);  // values or not: the more blocks
-    return (size_t)rope_blocks(T, p.segs, info.sm_count, kRopeBwdBlocksPerSm) * 2 * D * sizeof(float);
+    // with values or without: the more blocks
+    return (size_t)rope_blocks(T, RopeSplit(Hq, Hkv, D, kRopeBwdRows, true), info.sm_count) * 2 * D * sizeof(float);
 }
 
 extern "C" int swaa_qk_norm_rope_backward(const void* q, const void* k, long long q_stride, long long k_stride, const void* dq_out,
@@ -167,8 +158,7 @@ extern "C" int swaa_qk_norm_rope_backward(const void* q, const void* k, long lon
     DeviceInfo info;
     if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
     RopeGradParams p = {};
-    rope_segments(&p, Hq, Hkv, D, kRopeBwdRows, dv != nullptr);
-    const unsigned blocks = rope_blocks(T, p.segs, info.sm_count, kRopeBwdBlocksPerSm);
+    const unsigned blocks = rope_blocks(T, RopeSplit(Hq, Hkv, D, kRopeBwdRows, dv != nullptr), info.sm_count);
     const bool weights = q_weight != nullptr || k_weight != nullptr;
     if (weights && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < (size_t)blocks * 2 * D * sizeof(float)))
         return SWAA_ERR_WORKSPACE;
@@ -197,7 +187,9 @@ extern "C" int swaa_qk_norm_rope_backward(const void* q, const void* k, long lon
     p.partial = weights ? static_cast<float*>(workspace) : nullptr;
     auto* kernel = D == 128 ? (interleaved ? rope_backward_kernel<128, true> : rope_backward_kernel<128, false>)
                             : (interleaved ? rope_backward_kernel<64, true> : rope_backward_kernel<64, false>);
-    rc = launch_overlapped(kernel, dim3(blocks), kRopeThreads, 0, st, p);
+    static std::atomic<bool> attr_done[4][64];
+    if (ensure_dynamic_smem(kernel, kRopeSmem, attr_done[(D == 128 ? 2 : 0) + (interleaved ? 1 : 0)]) != SWAA_OK) return SWAA_ERR_CUDA;
+    rc = launch_overlapped(kernel, dim3(blocks), kRopeThreads, kRopeSmem, st, p);
     if (rc != SWAA_OK || !weights) return rc;
     return launch_overlapped(rope_weight_grad_kernel, dim3((unsigned)(2 * D / 32)), 1024, 0, st, p.partial, (int)blocks, D, dq_weight, dk_weight);
 }

@@ -15,8 +15,7 @@
 //
 // What bounds it: memory, every channel read and written once (2 * 2 bytes a channel; the gradient 3 * 2).  A head is D / 16 lanes,
 // each with two 16-byte pieces that hold both channels of its pairs, so the rotation needs no exchange and the norm log2(D / 16)
-// shuffles.  A warp takes kRopeRows groups of 32 / (D / 16) heads of one kind (query, key, value) of one token, all
-// its loads in flight at once; the frequencies of a token are spread over the lanes that hold the same channels of different heads,
+// shuffles.  A warp takes kRopeRows groups of 32 / (D / 16) heads (1 KiB) of one token after another; these shares come by bulk copies through a ring in shared memory.  The frequencies of a token are spread over the lanes that hold the same channels of different heads,
 // so that a lane forms 8 / (heads per group) of its 8 angles and takes the others by shuffle.
 #pragma once
 
@@ -27,8 +26,49 @@ namespace swaa {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kRopeRows = 4;     // groups of heads that a warp has in flight: forward
-constexpr int kRopeBwdRows = 2;  // and gradient, which holds two rows of each
+constexpr int kRopeRows = 4;     // groups of heads of a warp's share of a token: forward
+constexpr int kRopeBwdRows = 2;  // and gradient, which takes two rows of each head
+constexpr int kRopeShare = kRopeRows * 1024;  // bytes of a share: a group is 4 heads of 128 channels or 8 of 64
+constexpr int kRopeStages = 2;   // shares of a warp in shared memory
+constexpr int kRopeSmem = kRopeWarps * kRopeStages * kRopeShare;
+static_assert(kRopeBwdRows * 2 == kRopeRows, "the gradient's two inputs fill a share");
+
+// Work of a token: its heads in groups of 32 / (D / 16), a share of `rows` groups for every warp.  Shares hold query groups, or key and
+// value groups in turn, so that those with values, which are only copied, are about as long as the others.
+struct RopeSplit {
+    int groups_q, groups_kv;  // groups of query heads; of key heads and, where there are any, value heads
+    int seg_q, segs;          // shares of query groups, of all
+    bool values;
+    __host__ __device__ RopeSplit(int Hq, int Hkv, int D, int rows, bool with_values) {
+        const int per = 32 / (D / 16);
+        values = with_values;
+        groups_q = (Hq + per - 1) / per;
+        groups_kv = (Hkv + per - 1) / per * (values ? 2 : 1);
+        seg_q = (groups_q + rows - 1) / rows;
+        segs = seg_q + (groups_kv + rows - 1) / rows;
+    }
+};
+// A warp's place among them: share `seg` of the tokens stream, stream + streams, ...  Neighbouring warps have the shares of one token, which
+// are neighbours in memory.
+template <int D, int kRows>
+struct RopeWarp {
+    static constexpr int kHeads = 32 / (D / 16);
+    int seg, stream, streams, groups;
+    bool keys;  // keys and values
+    __device__ __forceinline__ RopeWarp(const RopeSplit& p, unsigned warp, unsigned warps) {
+        seg = (int)(warp % (unsigned)p.segs);
+        stream = (int)(warp / (unsigned)p.segs);
+        streams = (int)(warps / (unsigned)p.segs);
+        keys = seg >= p.seg_q;
+        groups = keys ? min(kRows, p.groups_kv - (seg - p.seg_q) * kRows) : min(kRows, p.groups_q - seg * kRows);
+    }
+    // group u of the share: whether it holds values, and its first head
+    __device__ __forceinline__ bool value(const RopeSplit& p, int u) const { return keys && p.values && ((seg - p.seg_q) * kRows + u) % 2 != 0; }
+    __device__ __forceinline__ int head(const RopeSplit& p, int u) const {
+        const int g = (keys ? seg - p.seg_q : seg) * kRows + u;
+        return (keys && p.values ? g / 2 : g) * kHeads;
+    }
+};
 
 struct RopeParams {
     const __nv_bfloat16 *q, *k, *v;              // [T, heads, D] with a stride between tokens
@@ -38,7 +78,6 @@ struct RopeParams {
     const float* inv_freq;                       // [rot / 2]
     const int32_t* positions;                    // [T]; cache form: may be null
     int T, Hq, Hkv, rot;
-    int seg_q, seg_k, segs;                      // warps' shares of a token's query heads, key heads, all
     __nv_bfloat16 *q_out, *k_out, *v_out;        // packed [T, heads, D]; cache form: k_out, v_out are the cache
     // cache form
     const int32_t *cu, *seqlens, *block_table;   // block_table null: dense [B, rows, Hkv, D]
@@ -55,7 +94,6 @@ struct RopeGradParams {
     const float* inv_freq;
     const int32_t* positions;
     int T, Hq, Hkv, rot;
-    int seg_q, seg_k, segs;
     __nv_bfloat16 *dq, *dk, *dv;
     long long dq_stride, dk_stride, dv_stride;
     float* partial;                              // [blocks][2][D]: weight gradients of a block
@@ -197,152 +235,223 @@ __device__ __forceinline__ RopeToken rope_token(const RopeParams& p, int t, int 
     return r;
 }
 
-// Asks for a warp's share of a token ahead of its use, one 128-byte line per lane.
-__device__ __forceinline__ void rope_prefetch(const __nv_bfloat16* share, int channels, int lane) {
-    if (64 * lane < channels) asm volatile("prefetch.global.L2 [%0];" ::"l"(share + 64 * lane));
+// A warp's ring of shares: bulk copies land in shared memory while earlier shares are worked on, so the bytes in flight do not
+// depend on registers.  Waits are bounded; a warp that gives up waits (again with a limit) for its copies in flight.
+struct RopeRing {
+    uint32_t data, bars;
+    volatile int* abort_flag;
+    int stage;
+    uint32_t phase;
+    __device__ __forceinline__ RopeRing(uint32_t smem, uint64_t* bar_words, volatile int* flag, int warp, int lane) {
+        data = smem + (uint32_t)(warp * kRopeStages * kRopeShare);
+        bars = smem_u32(bar_words + warp * kRopeStages);
+        abort_flag = flag;
+        stage = 0;
+        phase = 0;
+        if (lane == 0) {
+            for (int i = 0; i < kRopeStages; ++i) mbar_init(bars + 8u * (uint32_t)i, 1u);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        }
+        __syncwarp();
+    }
+    // One lane: announces `bytes` to come into stage i; copies (16-byte aligned, a multiple of 16 bytes) into its `at`-th byte.
+    __device__ __forceinline__ void expect(int i, uint32_t bytes) const { mbar_arrive_expect_tx(bars + 8u * (uint32_t)i, bytes); }
+    __device__ __forceinline__ void copy(int i, int at, const void* src, uint32_t bytes) const {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(data + (uint32_t)(i * kRopeShare + at)),
+                     "l"(src), "r"(bytes), "r"(bars + 8u * (uint32_t)i)
+                     : "memory");
+    }
+    __device__ __forceinline__ bool wait() const { return __all_sync(0xffffffffu, mbar_wait(bars + 8u * (uint32_t)stage, phase, abort_flag)) != 0; }
+    __device__ __forceinline__ uint32_t share() const { return data + (uint32_t)(stage * kRopeShare); }
+    __device__ __forceinline__ void next() {
+        if (++stage == kRopeStages) {
+            stage = 0;
+            phase ^= 1u;
+        }
+    }
+    // After a wait that ran out at the present share, with `ahead` shares filled from there on.
+    __device__ __forceinline__ void drain(int ahead) {
+        const uint64_t t0 = global_timer_ns();
+        for (; ahead > 0; --ahead, next())
+            while (!mbar_try_wait(bars + 8u * (uint32_t)stage, phase) && global_timer_ns() - t0 < kWaitLimitNs) {
+            }
+    }
+};
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 template <int D, bool kPairs, bool kCache>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
     using L = RopeLane<D, kPairs>;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
+    __shared__ uint64_t bar_words[kRopeWarps * kRopeStages];
+    __shared__ int abort_word;
+    if (threadIdx.x == 0) abort_word = 0;
+    __syncthreads();
     grid_wait();
     const int lane = threadIdx.x & 31;
-    const unsigned warp = blockIdx.x * kRopeWarps + (threadIdx.x >> 5), warps = gridDim.x * kRopeWarps;
-    const int seg = (int)(warp % (unsigned)p.segs), stream = (int)(warp / (unsigned)p.segs), streams = (int)(warps / (unsigned)p.segs);
+    const RopeSplit split(p.Hq, p.Hkv, D, kRopeRows, p.v != nullptr);
+    const RopeWarp<D, kRopeRows> me(split, blockIdx.x * kRopeWarps + (threadIdx.x >> 5), gridDim.x * kRopeWarps);
+    const int stream = me.stream, streams = me.streams;
     if (stream >= streams) return;
-    const int kind = seg < p.seg_q ? 0 : seg < p.seg_q + p.seg_k ? 1 : 2;
-    const int heads = kind == 0 ? p.Hq : p.Hkv;
-    const int h0 = (seg - (kind == 0 ? 0 : kind == 1 ? p.seg_q : p.seg_q + p.seg_k)) * (L::kHeads * kRopeRows);
-    const __nv_bfloat16* in = kind == 0 ? p.q : kind == 1 ? p.k : p.v;
-    const long long stride = kind == 0 ? p.q_stride : kind == 1 ? p.k_stride : p.v_stride;
-    __nv_bfloat16* out = kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out;
-    const float* w = kind == 0 ? p.qw : kind == 1 ? p.kw : nullptr;
-    const L ln(lane, p.inv_freq, kind == 2 ? 0 : p.rot);
+    const int heads = me.keys ? p.Hkv : p.Hq;
+    const float* w = me.keys ? p.kw : p.qw;
+    const L ln(lane, p.inv_freq, p.rot);
     const bool norm = w != nullptr;
     float wa[8], wb[8];
     load_weights(w, ln.a0, wa);
     load_weights(w, ln.b0, wb);
-    const int share = min(heads - h0, L::kHeads * kRopeRows) * D;
-    for (int t = stream; t < p.T; t += streams) {
-        if (t < p.T - streams) rope_prefetch(in + (t + streams) * stride + (long long)h0 * D, share, lane);
-        uint4 xa[kRopeRows], xb[kRopeRows];
+    RopeRing ring(smem_u32(smem_raw), bar_words, &abort_word, (int)threadIdx.x >> 5, lane);
+    uint32_t bytes = 0;  // of a share
+#pragma unroll
+    for (int u = 0; u < kRopeRows; ++u)
+        if (u < me.groups) bytes += (uint32_t)(min(heads - me.head(split, u), L::kHeads) * D * 2);
+    auto fill = [&](int i, long long t) {
+        ring.expect(i, bytes);
 #pragma unroll
         for (int u = 0; u < kRopeRows; ++u) {
-            const int h = h0 + u * L::kHeads + ln.sub;
-            if (h < heads) {
-                const __nv_bfloat16* x = in + t * stride + (long long)h * D;
-                xa[u] = *reinterpret_cast<const uint4*>(x + ln.a0);
-                xb[u] = *reinterpret_cast<const uint4*>(x + ln.b0);
-            } else {
-                xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
-            }
+            if (u >= me.groups) break;
+            const int h0 = me.head(split, u);
+            const __nv_bfloat16* src = !me.keys ? p.q + t * p.q_stride : me.value(split, u) ? p.v + t * p.v_stride : p.k + t * p.k_stride;
+            ring.copy(i, u * 1024, src + (long long)h0 * D, (uint32_t)(min(heads - h0, L::kHeads) * D * 2));
         }
+    };
+    int filled = 0;  // shares from the present one on
+    for (int t = stream; filled < kRopeStages && t < p.T; t += streams, ++filled)
+        if (lane == 0) fill(filled, t);
+    bool ok = true;
+    for (int t = stream; t < p.T; t += streams) {
         int position = 0;
         long long row = t;
+        bool store = true;
         if (kCache) {
             const RopeToken at = rope_token(p, t, lane);  // the same for the whole warp
-            if (!at.valid) continue;
             position = at.position;
-            if (kind != 0) row = at.row;
-            if (row < 0) continue;
-        } else if (kind != 2) {
+            if (me.keys) row = at.row;
+            store = at.valid && row >= 0;
+        } else {
             position = p.positions[t];
         }
         float c[8], s[8];
-        if (kind != 2) ln.turn(position, c, s);
+        ln.turn(position, c, s);
+        ok = ring.wait();
+        if (!ok) break;
+        if (store) {
 #pragma unroll
-        for (int u = 0; u < kRopeRows; ++u) {
-            if (h0 + u * L::kHeads >= heads) break;  // uniform
-            const int h = h0 + u * L::kHeads + ln.sub;
-            if (kind != 2) {
-                float a[8], b[8];
-                unpack_bf16x8(xa[u], a);
-                unpack_bf16x8(xb[u], b);
-                if (norm) {
-                    float ss = 0.f;
+            for (int u = 0; u < kRopeRows; ++u) {
+                if (u >= me.groups) break;  // uniform
+                const bool value = me.value(split, u);
+                const int h = me.head(split, u) + ln.sub;
+                const bool on = h < heads;
+                const uint32_t x = ring.share() + (uint32_t)(u * 1024 + (on ? ln.sub : 0) * D * 2);
+                uint4 va = ld_shared_v4(x + 2u * (uint32_t)ln.a0), vb = ld_shared_v4(x + 2u * (uint32_t)ln.b0);
+                if (!value) {
+                    float a[8], b[8];
+                    unpack_bf16x8(va, a);
+                    unpack_bf16x8(vb, b);
+                    if (norm) {
+                        float ss = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
-                    const float r = rsqrtf(L::sum(ss) * (1.f / D) + p.eps);
+                        for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
+                        const float r = rsqrtf(L::sum(ss) * (1.f / D) + p.eps);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        a[i] *= r * wa[i];
-                        b[i] *= r * wb[i];
+                        for (int i = 0; i < 8; ++i) {
+                            a[i] *= r * wa[i];
+                            b[i] *= r * wb[i];
+                        }
                     }
+                    ln.template rotate<false>(a, b, c, s);
+                    va = pack_bf16x8(a);
+                    vb = pack_bf16x8(b);
                 }
-                ln.template rotate<false>(a, b, c, s);
-                xa[u] = pack_bf16x8(a);
-                xb[u] = pack_bf16x8(b);
-            }
-            if (h < heads) {
-                __nv_bfloat16* y = out + (row * heads + h) * D;
-                *reinterpret_cast<uint4*>(y + ln.a0) = xa[u];
-                *reinterpret_cast<uint4*>(y + ln.b0) = xb[u];
+                if (on) {
+                    __nv_bfloat16* y = (!me.keys ? p.q_out : value ? p.v_out : p.k_out) + (row * heads + h) * D;
+                    *reinterpret_cast<uint4*>(y + ln.a0) = va;
+                    *reinterpret_cast<uint4*>(y + ln.b0) = vb;
+                }
             }
         }
+        __syncwarp();  // the share has been read
+        const long long ahead = (long long)t + (long long)kRopeStages * streams;
+        if (ahead < p.T) {
+            if (lane == 0) fill(ring.stage, ahead);
+        } else {
+            --filled;
+        }
+        ring.next();
     }
+    if (!ok) ring.drain(filled);
 }
 
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const RopeGradParams p) {
     using L = RopeLane<D, kPairs>;
+    extern __shared__ __align__(128) uint8_t smem_raw[];
     __shared__ float sm_w[kRopeWarps][D];
+    __shared__ uint64_t bar_words[kRopeWarps * kRopeStages];
+    __shared__ int abort_word;
+    if (threadIdx.x == 0) abort_word = 0;
+    __syncthreads();
     grid_wait();
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const unsigned warp = blockIdx.x * kRopeWarps + wid, warps = gridDim.x * kRopeWarps;
-    const int seg = (int)(warp % (unsigned)p.segs), stream = (int)(warp / (unsigned)p.segs), streams = (int)(warps / (unsigned)p.segs);
-    const int kind = seg < p.seg_q ? 0 : seg < p.seg_q + p.seg_k ? 1 : 2;
-    const int heads = kind == 0 ? p.Hq : p.Hkv;
-    const int h0 = (seg - (kind == 0 ? 0 : kind == 1 ? p.seg_q : p.seg_q + p.seg_k)) * (L::kHeads * kRopeBwdRows);
-    const __nv_bfloat16* x_in = kind == 0 ? p.q : p.k;
-    const long long x_stride = kind == 0 ? p.q_stride : p.k_stride;
-    const __nv_bfloat16* dy_in = kind == 0 ? p.dq_out : kind == 1 ? p.dk_out : p.dv_out;
-    __nv_bfloat16* dx = kind == 0 ? p.dq : kind == 1 ? p.dk : p.dv;
-    const long long dx_stride = kind == 0 ? p.dq_stride : kind == 1 ? p.dk_stride : p.dv_stride;
-    const float* w = kind == 0 ? p.qw : kind == 1 ? p.kw : nullptr;
-    const L ln(lane, p.inv_freq, kind == 2 ? 0 : p.rot);
+    const RopeSplit split(p.Hq, p.Hkv, D, kRopeBwdRows, p.dv != nullptr);
+    const RopeWarp<D, kRopeBwdRows> me(split, blockIdx.x * kRopeWarps + wid, gridDim.x * kRopeWarps);
+    const int heads = me.keys ? p.Hkv : p.Hq, streams = me.streams;
+    const float* w = me.keys ? p.kw : p.qw;
+    const L ln(lane, p.inv_freq, p.rot);
     const bool norm = w != nullptr;
     float wa[8], wb[8], da[8], db[8];
     load_weights(w, ln.a0, wa);
     load_weights(w, ln.b0, wb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) da[i] = db[i] = 0.f;
-    const int share = min(heads - h0, L::kHeads * kRopeBwdRows) * D;
-    for (int t = stream; t < p.T && stream < streams; t += streams) {
-        if (t < p.T - streams) {
-            rope_prefetch(dy_in + ((long long)(t + streams) * heads + h0) * D, share, lane);
-            if (norm) rope_prefetch(x_in + (t + streams) * x_stride + (long long)h0 * D, share, lane);
-        }
-        uint4 ya[kRopeBwdRows], yb[kRopeBwdRows], xa[kRopeBwdRows], xb[kRopeBwdRows];
+    RopeRing ring(smem_u32(smem_raw), bar_words, &abort_word, wid, lane);
+    uint32_t bytes = 0;  // of a share
+#pragma unroll
+    for (int u = 0; u < kRopeBwdRows; ++u)
+        if (u < me.groups) bytes += (uint32_t)(min(heads - me.head(split, u), L::kHeads) * D * 2) * (norm && !me.value(split, u) ? 2u : 1u);
+    auto fill = [&](int i, long long t) {
+        ring.expect(i, bytes);
 #pragma unroll
         for (int u = 0; u < kRopeBwdRows; ++u) {
-            const int h = h0 + u * L::kHeads + ln.sub;
-            ya[u] = yb[u] = xa[u] = xb[u] = make_uint4(0, 0, 0, 0);
-            if (h < heads) {
-                const __nv_bfloat16* y = dy_in + ((long long)t * heads + h) * D;
-                ya[u] = *reinterpret_cast<const uint4*>(y + ln.a0);
-                yb[u] = *reinterpret_cast<const uint4*>(y + ln.b0);
-                if (norm) {
-                    const __nv_bfloat16* x = x_in + t * x_stride + (long long)h * D;
-                    xa[u] = *reinterpret_cast<const uint4*>(x + ln.a0);
-                    xb[u] = *reinterpret_cast<const uint4*>(x + ln.b0);
-                }
-            }
+            if (u >= me.groups) break;
+            const int h0 = me.head(split, u);
+            const bool value = me.value(split, u);
+            const uint32_t n = (uint32_t)(min(heads - h0, L::kHeads) * D * 2);
+            ring.copy(i, u * 1024, (!me.keys ? p.dq_out : value ? p.dv_out : p.dk_out) + (t * heads + h0) * D, n);
+            if (norm && !value) ring.copy(i, kRopeShare / 2 + u * 1024, (me.keys ? p.k + t * p.k_stride : p.q + t * p.q_stride) + (long long)h0 * D, n);
         }
+    };
+    const int T = me.stream < streams ? p.T : 0;  // warps beyond the streams have no tokens
+    int filled = 0;
+    for (int t = me.stream; filled < kRopeStages && t < T; t += streams, ++filled)
+        if (lane == 0) fill(filled, t);
+    bool ok = true;
+    for (int t = me.stream; t < T; t += streams) {
         float c[8], s[8];
-        if (kind != 2) ln.turn(p.positions[t], c, s);
+        ln.turn(p.positions[t], c, s);
+        ok = ring.wait();
+        if (!ok) break;
 #pragma unroll
         for (int u = 0; u < kRopeBwdRows; ++u) {
-            if (h0 + u * L::kHeads >= heads) break;  // uniform
-            const int h = h0 + u * L::kHeads + ln.sub;
-            if (kind != 2) {
+            if (u >= me.groups) break;  // uniform
+            const bool value = me.value(split, u);
+            const int h = me.head(split, u) + ln.sub;
+            const bool on = h < heads;
+            const uint32_t from = ring.share() + (uint32_t)(u * 1024 + (on ? ln.sub : 0) * D * 2), oa = 2u * (uint32_t)ln.a0, ob = 2u * (uint32_t)ln.b0;
+            uint4 va = ld_shared_v4(from + oa), vb = ld_shared_v4(from + ob);
+            if (!value) {
                 float ga[8], gb[8];
-                unpack_bf16x8(ya[u], ga);
-                unpack_bf16x8(yb[u], gb);
+                unpack_bf16x8(va, ga);
+                unpack_bf16x8(vb, gb);
                 ln.template rotate<true>(ga, gb, c, s);
                 if (norm) {
                     float a[8], b[8], ss = 0.f;
-                    unpack_bf16x8(xa[u], a);
-                    unpack_bf16x8(xb[u], b);
+                    unpack_bf16x8(ld_shared_v4(from + kRopeShare / 2 + oa), a);
+                    unpack_bf16x8(ld_shared_v4(from + kRopeShare / 2 + ob), b);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) ss += a[i] * a[i] + b[i] * b[i];
                     const float r = rsqrtf(L::sum(ss) * (1.f / D) + p.eps);
@@ -351,8 +460,8 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const Ro
                     for (int i = 0; i < 8; ++i) {
                         a[i] *= r;
                         b[i] *= r;
-                        da[i] += ga[i] * a[i];  // rows past the last head hold zeros
-                        db[i] += gb[i] * b[i];
+                        da[i] += on ? ga[i] * a[i] : 0.f;
+                        db[i] += on ? gb[i] * b[i] : 0.f;
                         ga[i] *= wa[i];
                         gb[i] *= wb[i];
                         dot += ga[i] * a[i] + gb[i] * b[i];
@@ -364,16 +473,25 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const Ro
                         gb[i] = r * (gb[i] - b[i] * dot);
                     }
                 }
-                ya[u] = pack_bf16x8(ga);
-                yb[u] = pack_bf16x8(gb);
+                va = pack_bf16x8(ga);
+                vb = pack_bf16x8(gb);
             }
-            if (h < heads) {
-                __nv_bfloat16* x = dx + t * dx_stride + (long long)h * D;
-                *reinterpret_cast<uint4*>(x + ln.a0) = ya[u];
-                *reinterpret_cast<uint4*>(x + ln.b0) = yb[u];
+            if (on) {
+                __nv_bfloat16* x = (!me.keys ? p.dq + t * p.dq_stride : value ? p.dv + t * p.dv_stride : p.dk + t * p.dk_stride) + (long long)h * D;
+                *reinterpret_cast<uint4*>(x + ln.a0) = va;
+                *reinterpret_cast<uint4*>(x + ln.b0) = vb;
             }
         }
+        __syncwarp();  // the share has been read
+        const long long ahead = (long long)t + (long long)kRopeStages * streams;
+        if (ahead < T) {
+            if (lane == 0) fill(ring.stage, ahead);
+        } else {
+            --filled;
+        }
+        ring.next();
     }
+    if (!ok) ring.drain(filled);
     if (p.partial == nullptr) return;
     // weight gradients: the lanes with the same channels, then the block's warps in order, then (the next kernel) the blocks in order
 #pragma unroll
@@ -392,8 +510,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const Ro
     for (int i = threadIdx.x; i < 2 * D; i += kRopeThreads) {
         float sum = 0.f;
         for (int o = 0; o < kRopeWarps; ++o) {
-            const int sg = (int)((blockIdx.x * kRopeWarps + o) % (unsigned)p.segs);
-            if ((sg < p.seg_q ? 0 : sg < p.seg_q + p.seg_k ? 1 : 2) == i / D) sum += sm_w[o][i % D];
+            if ((RopeWarp<D, kRopeBwdRows>(split, blockIdx.x * kRopeWarps + o, gridDim.x * kRopeWarps).keys ? 1 : 0) == i / D) sum += sm_w[o][i % D];
         }
         p.partial[(size_t)blockIdx.x * 2 * D + i] = sum;
     }
