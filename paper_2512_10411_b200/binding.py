@@ -602,40 +602,53 @@ def swaa_decode_static(q, kcache, vcache, out, seqlens, window: int, n_sink: int
 
 def _on_current_device(t, where: str):
     """Launches go to the current device: a tensor of another one is refused."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != torch.cuda.current_device():
+    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"{where}: tensors must be on the current device")
 
 
-def _token_rows(t, H: int, D: int, name: str):
+def _dense(t, shape: tuple, dtype, where: str, name: str):
+    """Device address of a contiguous tensor of this shape and type (None stays None)."""
+    if t is None:
+        return None
+    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    _shaped(t, shape, where, name)  # one of these says what is wrong
+    return _dev_ptr(t, dtype, name)
+
+
+def _token_rows(t, shape: tuple, where: str, name: str):
     """(address, elements between tokens) of a bf16 tensor [T, H, D] whose heads and channels are dense."""
     if t is None:
-        return None, H * D
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        return None, shape[1] * shape[2]
+    _shaped(t, shape, where, name)
+    if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
-    if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+    T, H, D = shape
+    st, sh, sd = t.stride()
+    if sd != 1 or (sh != D and H > 1):
         raise ValueError(f"{name}: heads and channels must be dense")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else H * D
+    return t.data_ptr(), st if T > 1 else H * D
 
 
 def _shaped(t, shape, where: str, name: str):
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is not None and t.shape != shape:
         raise ValueError(f"{where}: {name} must be {list(shape)}")
 
 
-def _rope_args(where, q, k, v, q_weight, k_weight, inv_freq):
-    """Sizes of the rotation's arguments, checked: (T, Hq, Hkv, D, rotary_dim)."""
+def _rope_args(where, q, k, q_weight, k_weight, inv_freq):
+    """Sizes of the rotation's arguments, checked: (T, Hq, Hkv, D, addresses of the weights, of the frequencies, rotary_dim)."""
     _on_current_device(q, where)
     T, Hq, D = q.shape
-    Hkv = k.shape[1]
-    _shaped(k, (T, Hkv, D), where, "k")
-    _shaped(v, (T, Hkv, D), where, "v")
-    _shaped(q_weight, (D,), where, "q_weight")
-    _shaped(k_weight, (D,), where, "k_weight")
-    if inv_freq is not None and inv_freq.dim() != 1:
-        raise ValueError(f"{where}: inv_freq must be [rotary_dim / 2]")
-    return T, Hq, Hkv, D, 0 if inv_freq is None else 2 * inv_freq.numel()
+    f32 = torch.float32
+    rot = 0
+    if inv_freq is not None:
+        if inv_freq.dim() != 1:
+            raise ValueError(f"{where}: inv_freq must be [rotary_dim / 2]")
+        rot = 2 * inv_freq.numel()
+    return (T, Hq, k.shape[1], D, _dense(q_weight, (D,), f32, where, "q_weight"), _dense(k_weight, (D,), f32, where, "k_weight"),
+            _dev_ptr(inv_freq, f32, "inv_freq"), rot)
 
 
 def swaa_qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k_out, v_out, eps: float = 1e-6, interleaved: bool = False,
@@ -643,19 +656,14 @@ def swaa_qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k
     """Forwards to C swaa_qk_norm_rope.  q [T,Hq,D], k, v [T,Hkv,D] bf16, each with a stride of its own between tokens (slices of one
     projection's output); q_weight, k_weight f32 [D] or None (no norm); inv_freq f32 [rotary_dim / 2] or None (no rotation); positions
     int32 [T]; q_out [T,Hq,D], k_out, v_out [T,Hkv,D] bf16, contiguous.  v and v_out may both be None."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_qk_norm_rope"
-    T, Hq, Hkv, D, rot = _rope_args(where, q, k, v, q_weight, k_weight, inv_freq)
-    _shaped(positions, (T,), where, "positions")
-    _shaped(q_out, (T, Hq, D), where, "q_out")
-    _shaped(k_out, (T, Hkv, D), where, "k_out")
-    _shaped(v_out, (T, Hkv, D), where, "v_out")
-    bf, f32 = torch.bfloat16, torch.float32
-    (qp, qs), (kp, ks), (vp, vs) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k"), _token_rows(v, Hkv, D, "v")
-    rc = lib.swaa_qk_norm_rope(qp, kp, vp, qs, ks, vs, _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
-                               _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)), _dev_ptr(positions, torch.int32, "positions"), T,
-                               Hq, Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(k_out, bf, "k_out"), _dev_ptr(v_out, bf, "v_out"),
-                               _stream_ptr(stream))
+    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
+    bf, qs, ks = torch.bfloat16, (T, Hq, D), (T, Hkv, D)
+    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k"), _token_rows(v, ks, where, "v")
+    rc = lib.swaa_qk_norm_rope(qp, kp, vp, qn, kn, vn, qw, kw, float(eps), f, rot, int(bool(interleaved)),
+                               _dense(positions, (T,), torch.int32, where, "positions"), T, Hq, Hkv, D, _dense(q_out, qs, bf, where, "q_out"),
+                               _dense(k_out, ks, bf, where, "k_out"), _dense(v_out, ks, bf, where, "v_out"), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -671,20 +679,16 @@ def swaa_qk_norm_rope_backward(q, k, dq_out, dk_out, dv_out, q_weight, k_weight,
     dv_out: gradients of its outputs, contiguous; dq, dk, dv: those of its inputs, each with a stride of its own between tokens;
     dq_weight, dk_weight f32 [D] (None without the weight); workspace uint8 of qk_norm_rope_backward_workspace_size(T, Hq, Hkv, D) bytes
     (None without weights).  dv_out and dv may both be None."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_qk_norm_rope_backward"
-    T, Hq, Hkv, D, rot = _rope_args(where, dq_out, dk_out, dv_out, q_weight, k_weight, inv_freq)
-    for name, t, shp in (("q", q, (T, Hq, D)), ("k", k, (T, Hkv, D)), ("dq", dq, (T, Hq, D)), ("dk", dk, (T, Hkv, D)), ("dv", dv, (T, Hkv, D)),
-                         ("dq_weight", dq_weight, (D,)), ("dk_weight", dk_weight, (D,)), ("positions", positions, (T,))):
-        _shaped(t, shp, where, name)
-    bf, f32 = torch.bfloat16, torch.float32
-    (qp, qs), (kp, ks) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k")
-    (dqp, dqs), (dkp, dks), (dvp, dvs) = _token_rows(dq, Hq, D, "dq"), _token_rows(dk, Hkv, D, "dk"), _token_rows(dv, Hkv, D, "dv")
-    rc = lib.swaa_qk_norm_rope_backward(qp, kp, qs, ks, _dev_ptr(dq_out, bf, "dq_out"), _dev_ptr(dk_out, bf, "dk_out"), _dev_ptr(dv_out, bf, "dv_out"),
-                                        _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
-                                        _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)),
-                                        _dev_ptr(positions, torch.int32, "positions"), T, Hq, Hkv, D, dqp, dkp, dvp, dqs, dks, dvs,
-                                        _dev_ptr(dq_weight, f32, "dq_weight"), _dev_ptr(dk_weight, f32, "dk_weight"),
+    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, dq_out, dk_out, q_weight, k_weight, inv_freq)
+    bf, f32, qs, ks = torch.bfloat16, torch.float32, (T, Hq, D), (T, Hkv, D)
+    (qp, qn), (kp, kn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k")
+    (dqp, dqn), (dkp, dkn), (dvp, dvn) = _token_rows(dq, qs, where, "dq"), _token_rows(dk, ks, where, "dk"), _token_rows(dv, ks, where, "dv")
+    rc = lib.swaa_qk_norm_rope_backward(qp, kp, qn, kn, _dense(dq_out, qs, bf, where, "dq_out"), _dense(dk_out, ks, bf, where, "dk_out"),
+                                        _dense(dv_out, ks, bf, where, "dv_out"), qw, kw, float(eps), f, rot, int(bool(interleaved)),
+                                        _dense(positions, (T,), torch.int32, where, "positions"), T, Hq, Hkv, D, dqp, dkp, dvp, dqn, dkn, dvn,
+                                        _dense(dq_weight, (D,), f32, where, "dq_weight"), _dense(dk_weight, (D,), f32, where, "dk_weight"),
                                         _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
                                         _stream_ptr(stream))
     if rc != SWAA_OK:
@@ -692,20 +696,18 @@ def swaa_qk_norm_rope_backward(q, k, dq_out, dk_out, dv_out, q_weight, k_weight,
 
 
 def _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved):
-    """The arguments that swaa_cache_append and swaa_cache_append_paged pass on first, and their sizes."""
-    T, Hq, Hkv, D, rot = _rope_args(where, q, k, v, q_weight, k_weight, inv_freq)
+    """The arguments that swaa_cache_append and swaa_cache_append_paged pass on first, the address of q_out, and their sizes."""
+    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
     if v is None:
         raise ValueError(f"{where}: v is needed")
-    B = cu_seqlens_q.numel() - 1
-    if seqlens_k.numel() != B:
+    B = seqlens_k.numel()
+    i32, qs, ks = torch.int32, (T, Hq, D), (T, Hkv, D)
+    if cu_seqlens_q.numel() != B + 1:
         raise ValueError(f"{where}: cu_seqlens_q must be [B + 1] and seqlens_k [B]")
-    _shaped(q_out, (T, Hq, D), where, "q_out")
-    _shaped(positions, (T,), where, "positions")
-    f32, i32 = torch.float32, torch.int32
-    (qp, qs), (kp, ks), (vp, vs) = _token_rows(q, Hq, D, "q"), _token_rows(k, Hkv, D, "k"), _token_rows(v, Hkv, D, "v")
-    return (qp, kp, vp, qs, ks, vs, _dev_ptr(q_weight, f32, "q_weight"), _dev_ptr(k_weight, f32, "k_weight"), float(eps),
-            _dev_ptr(inv_freq, f32, "inv_freq"), rot, int(bool(interleaved)), _dev_ptr(positions, i32, "positions"),
-            _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k")), B, T, Hq, Hkv, D
+    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k"), _token_rows(v, ks, where, "v")
+    return (qp, kp, vp, qn, kn, vn, qw, kw, float(eps), f, rot, int(bool(interleaved)), _dense(positions, (T,), i32, where, "positions"),
+            _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k")), \
+        _dense(q_out, qs, torch.bfloat16, where, "q_out"), B, T, Hq, Hkv, D
 
 
 def swaa_cache_append(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, kcache, vcache, positions=None, window: int = 0,
@@ -713,15 +715,14 @@ def swaa_cache_append(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqle
     """Forwards to C swaa_cache_append.  q [Tq,Hq,D], k, v [Tq,Hkv,D] bf16 as in swaa_qk_norm_rope, packed by cu_seqlens_q int32 [B+1];
     seqlens_k int32 [B]: entries of each sequence including the new ones; q_out [Tq,Hq,D] bf16; kcache, vcache [B,Lmax,Hkv,D] bf16;
     positions int32 [Tq] or None (the entry's index); window > 0: the caches are rings as in trimmed_cache_slot."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_cache_append"
-    args, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved)
-    Lmax = kcache.shape[1]
-    _shaped(kcache, (B, Lmax, Hkv, D), where, "kcache")
-    _shaped(vcache, (B, Lmax, Hkv, D), where, "vcache")
-    bf = torch.bfloat16
-    rc = lib.swaa_cache_append(*args, B, T, Lmax, Hq, Hkv, D, int(window), int(n_sink), _dev_ptr(q_out, bf, "q_out"),
-                               _dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _stream_ptr(stream))
+    args, qo, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
+                                              interleaved)
+    bf, Lmax = torch.bfloat16, kcache.shape[1]
+    shape = (B, Lmax, Hkv, D)
+    rc = lib.swaa_cache_append(*args, B, T, Lmax, Hq, Hkv, D, int(window), int(n_sink), qo, _dense(kcache, shape, bf, where, "kcache"),
+                               _dense(vcache, shape, bf, where, "vcache"), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -730,20 +731,24 @@ def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q,
                             eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     """Forwards to C swaa_cache_append_paged: swaa_cache_append into kpages, vpages [num_pages,page_size,Hkv,D] bf16 through
     block_table int32 [B,max_blocks]."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_cache_append_paged"
-    args, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved)
-    num_pages, page_size = kpages.shape[:2]
-    _shaped(kpages, (num_pages, page_size, Hkv, D), where, "kpages")
-    _shaped(vpages, (num_pages, page_size, Hkv, D), where, "vpages")
-    if block_table.dim() != 2 or block_table.shape[0] != B:
-        raise ValueError(f"{where}: block_table must be [B, max_blocks]")
+    args, qo, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
+                                              interleaved)
     bf = torch.bfloat16
-    rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, block_table.shape[1], num_pages, page_size, Hq,
-                                     Hkv, D, _dev_ptr(q_out, bf, "q_out"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"),
-                                     _stream_ptr(stream))
+    num_pages, page_size = kpages.shape[:2]
+    shape = (num_pages, page_size, Hkv, D)
+    rows, max_blocks = _table_shape(block_table)
+    if rows != B:
+        raise ValueError(f"{where}: block_table must be [B, max_blocks]")
+    rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, max_blocks, num_pages, page_size, Hq, Hkv, D,
+                                     qo, _dense(kpages, shape, bf, where, "kpages"), _dense(vpages, shape, bf, where, "vpages"), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
+
+
+def _table_shape(block_table):
+    return block_table.shape if block_table.dim() == 2 else (-1, 0)
 
 
 def _weights_rows(where, weights_in, weights_out, B: int, Hkv: int) -> int:
@@ -868,15 +873,17 @@ def swaa_decode_weighted_paged(q, kpages, vpages, out, weights_in, weights_out, 
 
 
 def _evict_args(where, kcache, vcache, weights, seqlens, budget, kcache_out, vcache_out, weights_out, kept, seqlens_out):
-    """Sizes of an eviction's arguments, checked: (B, Hkv, D, budget, rows of weights, of weights_out)."""
+    """Sizes of an eviction's arguments and the addresses of those that both forms take."""
     _on_current_device(kcache, where)
-    B, Hkv, D = seqlens.numel(), kcache.shape[2], kcache.shape[3]
-    rows, rows_out = weights.shape[-1], weights_out.shape[-1]
-    for name, t, shp in (("vcache", vcache, kcache.shape), ("kcache_out", kcache_out, (*kcache_out.shape[:2], Hkv, D)),
-                         ("vcache_out", vcache_out, kcache_out.shape), ("weights", weights, (B, Hkv, rows)), ("weights_out", weights_out, (B, Hkv, rows_out)),
-                         ("kept", kept, (B, Hkv, int(budget))), ("seqlens_out", seqlens_out, (B,))):
-        _shaped(t, shp, where, name)
-    return B, Hkv, D, int(budget), rows, rows_out
+    B, (n, rows, Hkv, D), (n_out, rows_out, _, _) = seqlens.numel(), kcache.shape, kcache_out.shape
+    w_rows, wo_rows = weights.shape[-1], weights_out.shape[-1]
+    bf, f32, i32, shape, shape_out = torch.bfloat16, torch.float32, torch.int32, (n, rows, Hkv, D), (n_out, rows_out, Hkv, D)
+    inputs = (_dense(kcache, shape, bf, where, "kcache"), _dense(vcache, shape, bf, where, "vcache"), _dense(weights, (B, Hkv, w_rows), f32, where, "weights"),
+              _dev_ptr(seqlens, i32, "seqlens"))
+    caches = _dense(kcache_out, shape_out, bf, where, "kcache_out"), _dense(vcache_out, shape_out, bf, where, "vcache_out")
+    outputs = (_dense(weights_out, (B, Hkv, wo_rows), f32, where, "weights_out"), wo_rows, _dense(kept, (B, Hkv, budget), i32, where, "kept"),
+               _dense(seqlens_out, (B,), i32, where, "seqlens_out"))
+    return B, Hkv, D, w_rows, shape, shape_out, inputs, caches, outputs
 
 
 def swaa_cache_evict(kcache, vcache, weights, seqlens, budget: int, n_sink: int, recent: int, kcache_out, vcache_out, weights_out, kept,
@@ -884,17 +891,13 @@ def swaa_cache_evict(kcache, vcache, weights, seqlens, budget: int, n_sink: int,
     """Forwards to C swaa_cache_evict.  kcache, vcache [B,Lmax,Hkv,D] bf16; weights f32 [B,Hkv,>=seqlens]; seqlens int32 [B]; the first
     n_sink, the last `recent` and the heaviest of the other entries stay, `budget` in all, and go in order to kcache_out, vcache_out
     [B,>=budget,Hkv,D] bf16, weights_out f32 [B,Hkv,>=budget]; kept int32 [B,Hkv,budget]: their old index; seqlens_out int32 [B]."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_cache_evict"
-    B, Hkv, D, budget, rows, rows_out = _evict_args(where, kcache, vcache, weights, seqlens, budget, kcache_out, vcache_out, weights_out, kept,
-                                                    seqlens_out)
-    if kcache.shape[0] != B or kcache_out.shape[0] != B:
+    B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(where, kcache, vcache, weights, seqlens, int(budget), kcache_out, vcache_out,
+                                                                             weights_out, kept, seqlens_out)
+    if shape[0] != B or shape_out[0] != B:
         raise ValueError(f"{where}: caches must be [B, entries, Hkv, D]")
-    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
-    rc = lib.swaa_cache_evict(_dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _dev_ptr(weights, f32, "weights"),
-                              _dev_ptr(seqlens, i32, "seqlens"), B, kcache.shape[1], rows, Hkv, D, budget, int(n_sink), int(recent),
-                              _dev_ptr(kcache_out, bf, "kcache_out"), _dev_ptr(vcache_out, bf, "vcache_out"), kcache_out.shape[1],
-                              _dev_ptr(weights_out, f32, "weights_out"), rows_out, _dev_ptr(kept, i32, "kept"), _dev_ptr(seqlens_out, i32, "seqlens_out"),
+    rc = lib.swaa_cache_evict(*inputs, B, shape[1], rows, Hkv, D, int(budget), int(n_sink), int(recent), *caches, shape_out[1], *outputs,
                               _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
@@ -904,21 +907,17 @@ def swaa_cache_evict_paged(kpages, vpages, weights, seqlens, block_table, budget
                            block_table_out, weights_out, kept, seqlens_out, stream=None) -> None:
     """Forwards to C swaa_cache_evict_paged: swaa_cache_evict from pages [num_pages,page_size,Hkv,D] bf16 behind block_table int32
     [B,max_blocks] into pages behind block_table_out (of the same pool or another; none that the call reads)."""
-    lib = load_library()
+    lib = _lib or load_library()
     where = "swaa_cache_evict_paged"
-    B, Hkv, D, budget, rows, rows_out = _evict_args(where, kpages, vpages, weights, seqlens, budget, kpages_out, vpages_out, weights_out, kept,
-                                                    seqlens_out)
-    for name, t in (("block_table", block_table), ("block_table_out", block_table_out)):
-        if t.dim() != 2 or t.shape[0] != B:
-            raise ValueError(f"{where}: {name} must be [B, max_blocks]")
-    bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
-    rc = lib.swaa_cache_evict_paged(_dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"), _dev_ptr(weights, f32, "weights"),
-                                    _dev_ptr(seqlens, i32, "seqlens"), _dev_ptr(block_table, i32, "block_table"), B, block_table.shape[1],
-                                    kpages.shape[0], kpages.shape[1], rows, Hkv, D, budget, int(n_sink), int(recent),
-                                    _dev_ptr(kpages_out, bf, "kpages_out"), _dev_ptr(vpages_out, bf, "vpages_out"),
-                                    _dev_ptr(block_table_out, i32, "block_table_out"), block_table_out.shape[1], kpages_out.shape[0],
-                                    kpages_out.shape[1], _dev_ptr(weights_out, f32, "weights_out"), rows_out, _dev_ptr(kept, i32, "kept"),
-                                    _dev_ptr(seqlens_out, i32, "seqlens_out"), _stream_ptr(stream))
+    B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(where, kpages, vpages, weights, seqlens, int(budget), kpages_out, vpages_out,
+                                                                             weights_out, kept, seqlens_out)
+    (n, blocks), (n_out, blocks_out) = _table_shape(block_table), _table_shape(block_table_out)
+    if n != B or n_out != B:
+        raise ValueError(f"{where}: block_table and block_table_out must be [B, max_blocks]")
+    i32 = torch.int32
+    rc = lib.swaa_cache_evict_paged(*inputs, _dev_ptr(block_table, i32, "block_table"), B, blocks, shape[0], shape[1], rows, Hkv, D, int(budget),
+                                    int(n_sink), int(recent), *caches, _dev_ptr(block_table_out, i32, "block_table_out"), blocks_out, shape_out[0],
+                                    shape_out[1], *outputs, _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 

@@ -229,7 +229,7 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 // several thousand weights.
 static int evict_cluster(long long rows, int length, int sms) {
     int c = 1;
-    while (c < kEvictMaxCluster && 2 * c * rows <= sms && (length + 2 * c - 1) / (2 * c) >= kEvictTile / 2) c *= 2;
+    while (c < kEvictMaxCluster && 2 * c * rows <= sms && (length + 2 * c - 1) / (2 * c) >= kEvictShare) c *= 2;
     return c;
 }
 
@@ -258,7 +258,7 @@ static int evict_impl(EvictParams p, int D, bool paged, cudaStream_t st) {
     const int length = std::min(p.rows, p.weights_rows);
     const int ranks = evict_cluster((long long)heads, length, info.sm_count);
     constexpr int kMostKeys = 48 * 1024;
-    p.cap = std::min(((length + ranks - 1) / ranks + kEvictPerThread - 1) / kEvictPerThread * kEvictPerThread, kMostKeys);
+    p.cap = std::min(((length + ranks - 1) / ranks + 3) / 4 * 4, kMostKeys);
     static std::atomic<bool> attr_done[64];
     if (ensure_dynamic_smem(evict_select_kernel, kMostKeys * 4, attr_done) != SWAA_OK) return SWAA_ERR_CUDA;
     cudaLaunchAttribute attr[2];

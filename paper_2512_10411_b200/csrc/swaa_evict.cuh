@@ -38,9 +38,11 @@ struct EvictParams {
 constexpr int kEvictThreads = 1024;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictBins = 2048;
-constexpr int kEvictMaxCluster = 8;
-constexpr int kEvictPerThread = 4;  // neighbouring keys of a thread in the listing pass
-constexpr int kEvictTile = kEvictThreads * kEvictPerThread;
+// A row is cut over up to four blocks while each keeps 8192 weights.  One row of 8 heads, us with one, two, four and eight blocks: 32768
+// weights 27.4, 23.7, 22.8, -; 65536 -, 31.2, 27.0, 31.9; 131072 -, -, 33.4, 35.2 (an exchange between blocks takes about 1.5 us of a pass).
+constexpr int kEvictMaxCluster = 4;
+constexpr int kEvictShare = 8192;
+constexpr int kEvictBatch = 16;     // weights of a thread on their way at a time
 
 // Integers in the order of the weights: -0 and 0 are equal, NaN is above everything.
 __device__ __forceinline__ uint32_t evict_key(float w) {
@@ -48,6 +50,10 @@ __device__ __forceinline__ uint32_t evict_key(float w) {
     const uint32_t u = __float_as_uint(w + 0.f);
     return u ^ ((u >> 31) != 0u ? 0xffffffffu : 0x80000000u);
 }
+
+// The weight of a key, but for zeros and NaN, of which there are several.
+__device__ __forceinline__ bool evict_key_is_one(uint32_t k) { return k != 0x80000000u && k != 0xffffffffu; }
+__device__ __forceinline__ float evict_weight(uint32_t k) { return __uint_as_float((k >> 31) != 0u ? k ^ 0x80000000u : ~k); }
 
 // Inclusive sum over the block's threads; sm: kEvictWarps words.  Every thread calls it.
 __device__ __forceinline__ uint32_t evict_scan(uint32_t x, uint32_t* sm, uint32_t* total) {
@@ -73,9 +79,10 @@ __device__ __forceinline__ uint32_t evict_scan(uint32_t x, uint32_t* sm, uint32_
 
 __global__ void __launch_bounds__(kEvictThreads, 1) evict_select_kernel(const EvictParams p) {
     namespace cg = cooperative_groups;
-    extern __shared__ uint32_t sm_keys[];
+    extern __shared__ __align__(16) uint32_t sm_keys[];
     __shared__ uint32_t hist[3][kEvictBins];
     __shared__ uint32_t sm_scan[32], sm_gt, sm_eq, sm_bin, sm_above;
+    __shared__ uint2 sm_count[kEvictWarps];
     static_assert(kEvictWarps == 32, "one word per lane in evict_scan");
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -106,17 +113,24 @@ __global__ void __launch_bounds__(kEvictThreads, 1) evict_select_kernel(const Ev
         w_out[to] = w[from];
     }
     if (m == 0) return;
-    // this block's share of the candidates, a multiple of kEvictPerThread each
-    const int share = ((candidates + ranks - 1) / ranks + kEvictPerThread - 1) / kEvictPerThread * kEvictPerThread;
+    const int share = (candidates + ranks - 1) / ranks;  // of the candidates, this block's
     const int c0 = min(rank * share, candidates), cn = min(share, candidates - c0);
     const float* wc = w + p.n_sink + c0;
     auto key = [&](int i) -> uint32_t { return i < p.cap ? sm_keys[i] : evict_key(wc[i]); };
     for (int i = tid; i < 3 * kEvictBins; i += kEvictThreads) (&hist[0][0])[i] = 0u;
     __syncthreads();
-    for (int i = tid; i < cn; i += kEvictThreads) {  // the first pass reads the weights
-        const uint32_t k = evict_key(wc[i]);
-        if (i < p.cap) sm_keys[i] = k;
-        atomicAdd(&hist[0][k >> 21], 1u);
+    for (int i0 = tid; i0 < cn; i0 += kEvictBatch * kEvictThreads) {  // the first pass reads the weights, several on their way at a time
+        float x[kEvictBatch];
+#pragma unroll
+        for (int u = 0; u < kEvictBatch; ++u) x[u] = i0 + u * kEvictThreads < cn ? wc[i0 + u * kEvictThreads] : 0.f;
+#pragma unroll
+        for (int u = 0; u < kEvictBatch; ++u) {
+            const int i = i0 + u * kEvictThreads;
+            if (i >= cn) break;
+            const uint32_t k = evict_key(x[u]);
+            if (i < p.cap) sm_keys[i] = k;
+            atomicAdd(&hist[0][k >> 21], 1u);
+        }
     }
     // digits of the last survivor's key, from the top; `need` survivors share the digits found so far
     uint32_t prefix = 0, need = (uint32_t)m;
@@ -124,20 +138,40 @@ __global__ void __launch_bounds__(kEvictThreads, 1) evict_select_kernel(const Ev
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
         if (pass > 0) {
-            for (int i = tid; i < cn; i += kEvictThreads) {
-                const uint32_t k = key(i);
+            auto count = [&](uint32_t k) {
                 if ((k >> (shift + bits)) == prefix) atomicAdd(&hist[pass][(k >> shift) & ((1u << bits) - 1u)], 1u);
+            };
+            const int held = min(cn, p.cap) / 4;  // four keys at a time from shared memory, then the rest
+            for (int i = tid; i < held; i += kEvictThreads) {
+                const uint4 k = reinterpret_cast<const uint4*>(sm_keys)[i];
+                count(k.x);
+                count(k.y);
+                count(k.z);
+                count(k.w);
             }
+            for (int i = 4 * held + tid; i < cn; i += kEvictThreads) count(key(i));
         }
         if (ranks > 1) cluster.sync();
         else __syncthreads();
         // thread t: bins kEvictBins - 1 - 2 t and the one below it, so that the running sum counts from the top
         uint32_t c[2] = {0u, 0u};
         const int top = kEvictBins - 1 - 2 * tid;
-        for (int r = 0; r < ranks; ++r) {
-            const uint32_t* h = ranks > 1 ? cluster.map_shared_rank(&hist[pass][0], r) : &hist[pass][0];
-            c[0] += h[top];
-            c[1] += h[top - 1];
+        if (ranks == 1) {
+            c[0] = hist[pass][top];
+            c[1] = hist[pass][top - 1];
+        } else {
+            uint32_t x[2 * kEvictMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kEvictMaxCluster; ++r) {
+                const uint32_t* h = cluster.map_shared_rank(&hist[pass][0], r < ranks ? r : 0);
+                x[2 * r] = r < ranks ? h[top] : 0u;
+                x[2 * r + 1] = r < ranks ? h[top - 1] : 0u;
+            }
+#pragma unroll
+            for (int r = 0; r < kEvictMaxCluster; ++r) {
+                c[0] += x[2 * r];
+                c[1] += x[2 * r + 1];
+            }
         }
         uint32_t total;
         const uint32_t upto = evict_scan(c[0] + c[1], sm_scan, &total), before = upto - c[0] - c[1];
@@ -151,54 +185,62 @@ __global__ void __launch_bounds__(kEvictThreads, 1) evict_select_kernel(const Ev
         need -= sm_above;
         __syncthreads();
     }
-    // `prefix` is the key; survivors are all above it and the first `need` equal to it.  Where does this block's list start?
-    uint32_t gt0 = 0, eq0 = 0;
+    // `prefix` is the key; survivors are all above it and the first `need` equal to it.  A warp lists a stretch of the share, 32 keys
+    // at a time; how many there are before it is counted first.
+    const int lane = tid & 31, warp = tid >> 5;
+    const int stretch = ((cn + kEvictWarps - 1) / kEvictWarps + 127) / 128 * 128, i0 = min(warp * stretch, cn), i1 = min(i0 + stretch, cn);
+    uint32_t gt = 0, eq = 0;
+    auto tell = [&](uint32_t k) {
+        gt += k > prefix;
+        eq += k == prefix;
+    };
+    const int held = max(min(i1, p.cap) - i0, 0) / 4;
+    for (int i = lane; i < held; i += 32) {
+        const uint4 k = reinterpret_cast<const uint4*>(sm_keys + i0)[i];
+        tell(k.x);
+        tell(k.y);
+        tell(k.z);
+        tell(k.w);
+    }
+    for (int i = i0 + 4 * held + lane; i < i1; i += 32) tell(key(i));
+    gt = __reduce_add_sync(0xffffffffu, gt);
+    eq = __reduce_add_sync(0xffffffffu, eq);
+    if (lane == 0) sm_count[warp] = make_uint2(gt, eq);
+    __syncthreads();
+    const uint2 theirs = sm_count[lane];
+    uint32_t before_gt = lane < warp ? theirs.x : 0u, before_eq = lane < warp ? theirs.y : 0u, all_gt = theirs.x, all_eq = theirs.y;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        before_gt += __shfl_xor_sync(0xffffffffu, before_gt, o);
+        before_eq += __shfl_xor_sync(0xffffffffu, before_eq, o);
+        all_gt += __shfl_xor_sync(0xffffffffu, all_gt, o);
+        all_eq += __shfl_xor_sync(0xffffffffu, all_eq, o);
+    }
     if (ranks > 1) {
-        uint32_t gt = 0, eq = 0;
-        for (int i = tid; i < cn; i += kEvictThreads) {
-            const uint32_t k = key(i);
-            gt += k > prefix;
-            eq += k == prefix;
-        }
-        uint32_t total_gt, total_eq;
-        evict_scan(gt, sm_scan, &total_gt);
-        evict_scan(eq, sm_scan, &total_eq);
         if (tid == 0) {
-            sm_gt = total_gt;
-            sm_eq = total_eq;
+            sm_gt = all_gt;
+            sm_eq = all_eq;
         }
         cluster.sync();
         for (int r = 0; r < rank; ++r) {
-            gt0 += *cluster.map_shared_rank(&sm_gt, r);
-            eq0 += *cluster.map_shared_rank(&sm_eq, r);
+            before_gt += *cluster.map_shared_rank(&sm_gt, r);
+            before_eq += *cluster.map_shared_rank(&sm_eq, r);
         }
     }
-    for (int base = 0; base < cn; base += kEvictTile) {
-        const int i0 = base + kEvictPerThread * tid;
-        uint32_t k[kEvictPerThread], gt = 0, eq = 0;
-#pragma unroll
-        for (int e = 0; e < kEvictPerThread; ++e) {
-            k[e] = i0 + e < cn ? key(i0 + e) : 0u;
-            gt += i0 + e < cn && k[e] > prefix;
-            eq += i0 + e < cn && k[e] == prefix;
+    const unsigned below = (1u << lane) - 1u;
+#pragma unroll 4
+    for (int i = i0; i < i1; i += 32) {
+        const uint32_t k = i + lane < i1 ? key(i + lane) : 0u;
+        const bool above = i + lane < i1 && k > prefix, equal = i + lane < i1 && k == prefix;
+        const unsigned gts = __ballot_sync(0xffffffffu, above), eqs = __ballot_sync(0xffffffffu, equal);
+        const uint32_t q = before_eq + __popc(eqs & below);
+        if (above || (equal && q < need)) {
+            const int to = p.n_sink + (int)(before_gt + __popc(gts & below) + min(q, need));
+            kept[to] = p.n_sink + c0 + i + lane;
+            w_out[to] = evict_key_is_one(k) ? evict_weight(k) : wc[i + lane];
         }
-        uint32_t total;
-        const uint32_t before = evict_scan(gt << 16 | eq, sm_scan, &total) - (gt << 16 | eq);  // a tile has at most 4096 of each
-        uint32_t g = gt0 + (before >> 16), q = eq0 + (before & 0xffffu);
-#pragma unroll
-        for (int e = 0; e < kEvictPerThread; ++e) {
-            if (i0 + e >= cn) continue;
-            const bool above = k[e] > prefix, equal = k[e] == prefix;
-            if (above || (equal && q < need)) {
-                const int to = p.n_sink + (int)(g + min(q, need));
-                kept[to] = p.n_sink + c0 + i0 + e;
-                w_out[to] = wc[i0 + e];
-            }
-            g += above;
-            q += equal;
-        }
-        gt0 += total >> 16;
-        eq0 += total & 0xffffu;
+        before_gt += __popc(gts);
+        before_eq += __popc(eqs);
     }
     if (ranks > 1) cluster.sync();  // no block leaves while another reads its counts
 }

@@ -124,22 +124,22 @@ def test_workspace_sizes_of_refused_shapes(lib):
 
 def test_binding_refuses_shapes_and_kinds(lib):
     x = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
-    w, pos = torch.ones(64), torch.zeros(3, dtype=torch.int32)
+    w, pos, f = torch.ones(64), torch.zeros(3, dtype=torch.int32), torch.ones(32)
     with pytest.raises(TypeError, match="CUDA"):
-        swaa.swaa_qk_norm_rope(x, x, x, w, w, torch.ones(32), pos, x, x, x)
-    with pytest.raises(ValueError, match="k must be"):
-        swaa.swaa_qk_norm_rope(x, x[:2], None, w, w, torch.ones(32), pos, x, x, None)
+        swaa.swaa_qk_norm_rope(x, x, x, w, w, f, pos, x, x, x)
+    with pytest.raises(TypeError, match="CUDA"):
+        swaa.swaa_qk_norm_rope(x, x, x, None, None, None, pos, x, x, x)
     with pytest.raises(ValueError, match="q_weight must be"):
-        swaa.swaa_qk_norm_rope(x, x, None, w[:32], w, torch.ones(32), pos, x, x, None)
-    with pytest.raises(ValueError, match="positions must be"):
-        swaa.swaa_qk_norm_rope(x, x, None, w, w, torch.ones(32), pos[:2], x, x, None)
-    with pytest.raises(ValueError, match="dq_weight must be"):
-        swaa.swaa_qk_norm_rope_backward(x, x, x, x, None, w, w, torch.ones(32), pos, x, x, None, w[:3], w, None)
+        swaa.swaa_qk_norm_rope(x, x, None, w[:32], w, f, pos, x, x, None)
+    with pytest.raises(ValueError, match="inv_freq must be"):
+        swaa.swaa_qk_norm_rope(x, x, None, None, None, f[None], pos, x, x, None)
+    with pytest.raises(ValueError, match="q must be"):
+        swaa.swaa_qk_norm_rope_backward(x[:2], x, x, x, None, None, None, None, pos, x, x, None, None, None, None)
     cu = torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError, match="v is needed"):
-        swaa.swaa_cache_append(x, x, None, w, w, torch.ones(32), cu, cu[:2], x, x, x)
+        swaa.swaa_cache_append(x, x, None, None, None, None, cu, cu[:2], x, x, x)
     with pytest.raises(ValueError, match="seqlens_k"):
-        swaa.swaa_cache_append(x, x, x, w, w, torch.ones(32), cu, cu, x, x, x)
+        swaa.swaa_cache_append(x, x, x, None, None, None, cu, cu, x, x, x)
 
 
 def test_key_weights_workspace_grows_with_what_is_cut(lib):

@@ -184,3 +184,21 @@ def test_other_stream_and_graph():
         graph.replay()
         assert swaa.last_device_status() == 0
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_refused_tensors():
+    T, Hq, Hkv, D = 3, 4, 2, 64
+    qkv, (qw, kw), f, pos = make(T, Hq, Hkv, D, D, 12)
+    good = dict(zip(("q", "k", "v"), qkv.split((Hq, Hkv, Hkv), 1)))
+    good.update(q_weight=qw, k_weight=kw, inv_freq=f, positions=pos)
+    good.update({n: torch.empty(T, h, D, dtype=torch.bfloat16, device="cuda") for n, h in (("q_out", Hq), ("k_out", Hkv), ("v_out", Hkv))})
+    swaa.swaa_qk_norm_rope(**good)
+    bad = [(dict(k=good["k"][:2]), ValueError), (dict(v=good["v"][:, :1]), ValueError), (dict(positions=pos[:2]), ValueError), (dict(positions=pos.long()), TypeError),
+           (dict(q=good["q"].float()), TypeError), (dict(q=good["q"].cpu()), TypeError), (dict(q=good["q"].transpose(0, 1).contiguous().transpose(0, 1)), ValueError),
+           (dict(k_out=good["v_out"][:, :1]), ValueError), (dict(q_out=torch.empty(T, Hq, 2 * D, dtype=torch.bfloat16, device="cuda")[..., :D]), ValueError),
+           (dict(q_weight=qw.bfloat16()), TypeError), (dict(k_weight=kw[:32]), ValueError), (dict(v_out=None), swaa.SwaaError), (dict(inv_freq=f[:5]), swaa.SwaaError),
+           (dict(q=torch.empty(T, Hq * D + 4, dtype=torch.bfloat16, device="cuda")[:, :Hq * D].view(T, Hq, D)), swaa.SwaaError)]
+    for change, error in bad:
+        with pytest.raises(error):
+            swaa.swaa_qk_norm_rope(**{**good, **change})
+    assert swaa.last_device_status() == 0
