@@ -211,3 +211,29 @@ def test_graph_and_stream():
         run(1)
         assert torch.equal(w[0], w[1])
     assert swaa.last_device_status() == 0
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("mask", [(9, 9, True), (300, 130, False), (1000, 0, False)])
+@pytest.mark.parametrize("Hq,D,last", [(8, 64, 16), (16, 128, 64), (32, 128, 100), (4, 128, 0)])
+def test_blocks_of_several_key_tiles(Hq, D, last, mask, paged):
+    """Many sequences of which few queries count: a block goes through several tiles of keys, with its queries in place (up to two steps
+    of 128 channels) or loaded again, and past tiles that no query sees."""
+    Hkv, B = 4, 40
+    ctx = [2000 + 7 * i % 140 for i in range(B)]
+    ctx[3], ctx[17], ctx[18] = 1, 129, 1500
+    new = list(ctx) if last else [min(n, 1 + i % 60) for i, n in enumerate(ctx)]
+    s = make(new, ctx, Hq, Hkv, D, 12, paged)
+    w_out = torch.full((B, Hkv, max(ctx) + 3), 9.0, device="cuda")
+    call(s, None, w_out, mask, last)
+    assert swaa.last_device_status() == 0
+    check(s, new, ctx, None, w_out, mask, last, D ** -0.5)
+    if paged:  # a bad page in the middle of a run: its keys stay as they are, the others have what they had
+        t, before = s["table"].clone(), w_out.clone()
+        t[5, 6] = -1
+        w_out.fill_(9.0)
+        call({**s, "table": t}, None, w_out, mask, last)
+        assert swaa.status_str(swaa.last_device_status()) == "SWAA_ERR_BAD_SEQLENS"
+        assert (w_out[5, :, 768:896] == 9).all()
+        before[5, :, 768:896] = 9.0
+        assert torch.equal(w_out, before)
