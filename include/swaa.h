@@ -509,7 +509,8 @@ int swaa_cache_append_paged(const void* q, const void* k, const void* v, long lo
  *   workspace       at least swaa_key_weights_workspace_size(...) bytes (paged: max_seqlen_k = the smaller of max_blocks * page_size and
  *                   weights_rows), 256-byte aligned, uninitialised: sums of blocks that share the queries of a key.
  * A sequence with len_q > len_k, longer than the stated bounds or than weights_rows is reported as SWAA_ERR_BAD_SEQLENS through the
- * status word and gathers nothing; a page index outside [0, num_pages) likewise, for its keys.  Sums are taken in a fixed order.  Other
+ * status word and gathers nothing; a page index outside [0, num_pages) likewise, for its keys (pages whose keys no query of the call
+ * sees are not looked up).  Sums are taken in a fixed order.  Other
  * arguments and status codes as for swaa_prefill_chunked and swaa_prefill_paged.
  */
 size_t swaa_key_weights_workspace_size(int B, int max_seqlen_q, int max_seqlen_k, int Hq, int Hkv, int window, int n_sink,
@@ -573,6 +574,7 @@ int swaa_decode_weighted_paged(const void* q, const void* kpages, const void* vp
  *   kept            device, int32 [B, Hkv, budget]: their index in the old cache, ascending.  Entries of weights_out and kept from the new
  *                   length on are left as they are.
  *   seqlens_out     device, int32 [B]: min(seqlens[b], budget); not seqlens itself.
+ * B at most 65535.
  */
 int swaa_cache_evict(const void* kcache, const void* vcache, const float* weights, const int32_t* seqlens, int B, int Lmax,
                      int weights_rows, int Hkv, int D, int budget, int n_sink, int recent, void* kcache_out, void* vcache_out,

@@ -600,23 +600,29 @@ def swaa_decode_static(q, kcache, vcache, out, seqlens, window: int, n_sink: int
         raise SwaaError(rc, "swaa_decode_static")
 
 
-def _on_current_device(t, where: str):
-    """Launches go to the current device: a tensor of another one is refused."""
-    if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
+def _current_device(t, where: str) -> int:
+    """Index of the current device, which launches go to: a tensor of another one is refused."""
+    if not t.is_cuda:  # refused with the other arguments
+        return torch.cuda.current_device() if torch.cuda.is_initialized() else -1
+    dev = torch._C._cuda_getDevice()
+    if t.get_device() != dev:
         raise ValueError(f"{where}: tensors must be on the current device")
+    return dev
 
 
-def _dense(t, shape: tuple, dtype, where: str, name: str):
-    """Device address of a contiguous tensor of this shape and type (None stays None)."""
+def _dense(t, shape, dtype, where: str, name: str, dev: int):
+    """Device address of a contiguous tensor of this shape (None: any), type and device (None stays None)."""
     if t is None:
         return None
-    if t.shape == shape and t.dtype is dtype and t.is_cuda and t.is_contiguous():
+    if (shape is None or t.shape == shape) and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev >= 0:
         return t.data_ptr()
-    _shaped(t, shape, where, name)  # one of these says what is wrong
-    return _dev_ptr(t, dtype, name)
+    if shape is not None:
+        _shaped(t, shape, where, name)  # one of these says what is wrong
+    _dev_ptr(t, dtype, name)
+    raise ValueError(f"{where}: {name} must be on the current device")
 
 
-def _token_rows(t, shape: tuple, where: str, name: str):
+def _token_rows(t, shape: tuple, where: str, name: str, dev: int):
     """(address, elements between tokens) of a bf16 tensor [T, H, D] whose heads and channels are dense."""
     if t is None:
         return None, shape[1] * shape[2]
@@ -625,6 +631,8 @@ def _token_rows(t, shape: tuple, where: str, name: str):
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: {name} must be on the current device")
     T, H, D = shape
     st, sh, sd = t.stride()
     if sd != 1 or (sh != D and H > 1):
@@ -638,8 +646,9 @@ def _shaped(t, shape, where: str, name: str):
 
 
 def _rope_args(where, q, k, q_weight, k_weight, inv_freq):
-    """Sizes of the rotation's arguments, checked: (T, Hq, Hkv, D, addresses of the weights, of the frequencies, rotary_dim)."""
-    _on_current_device(q, where)
+    """What the rotation's calls have in common, checked: (device, T, Hq, Hkv, D, addresses of the weights, of the frequencies,
+    rotary_dim)."""
+    dev = _current_device(q, where)
     T, Hq, D = q.shape
     f32 = torch.float32
     rot = 0
@@ -647,8 +656,8 @@ def _rope_args(where, q, k, q_weight, k_weight, inv_freq):
         if inv_freq.dim() != 1:
             raise ValueError(f"{where}: inv_freq must be [rotary_dim / 2]")
         rot = 2 * inv_freq.numel()
-    return (T, Hq, k.shape[1], D, _dense(q_weight, (D,), f32, where, "q_weight"), _dense(k_weight, (D,), f32, where, "k_weight"),
-            _dev_ptr(inv_freq, f32, "inv_freq"), rot)
+    return (dev, T, Hq, k.shape[1], D, _dense(q_weight, (D,), f32, where, "q_weight", dev), _dense(k_weight, (D,), f32, where, "k_weight", dev),
+            _dense(inv_freq, None, f32, where, "inv_freq", dev), rot)
 
 
 def swaa_qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k_out, v_out, eps: float = 1e-6, interleaved: bool = False,
@@ -658,12 +667,13 @@ def swaa_qk_norm_rope(q, k, v, q_weight, k_weight, inv_freq, positions, q_out, k
     int32 [T]; q_out [T,Hq,D], k_out, v_out [T,Hkv,D] bf16, contiguous.  v and v_out may both be None."""
     lib = _lib or load_library()
     where = "swaa_qk_norm_rope"
-    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
+    dev, T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
     bf, qs, ks = torch.bfloat16, (T, Hq, D), (T, Hkv, D)
-    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k"), _token_rows(v, ks, where, "v")
+    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q", dev), _token_rows(k, ks, where, "k", dev), _token_rows(v, ks, where, "v", dev)
     rc = lib.swaa_qk_norm_rope(qp, kp, vp, qn, kn, vn, qw, kw, float(eps), f, rot, int(bool(interleaved)),
-                               _dense(positions, (T,), torch.int32, where, "positions"), T, Hq, Hkv, D, _dense(q_out, qs, bf, where, "q_out"),
-                               _dense(k_out, ks, bf, where, "k_out"), _dense(v_out, ks, bf, where, "v_out"), _stream_ptr(stream))
+                               _dense(positions, (T,), torch.int32, where, "positions", dev), T, Hq, Hkv, D,
+                               _dense(q_out, qs, bf, where, "q_out", dev),
+                               _dense(k_out, ks, bf, where, "k_out", dev), _dense(v_out, ks, bf, where, "v_out", dev), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -681,33 +691,34 @@ def swaa_qk_norm_rope_backward(q, k, dq_out, dk_out, dv_out, q_weight, k_weight,
     (None without weights).  dv_out and dv may both be None."""
     lib = _lib or load_library()
     where = "swaa_qk_norm_rope_backward"
-    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, dq_out, dk_out, q_weight, k_weight, inv_freq)
+    dev, T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, dq_out, dk_out, q_weight, k_weight, inv_freq)
     bf, f32, qs, ks = torch.bfloat16, torch.float32, (T, Hq, D), (T, Hkv, D)
-    (qp, qn), (kp, kn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k")
-    (dqp, dqn), (dkp, dkn), (dvp, dvn) = _token_rows(dq, qs, where, "dq"), _token_rows(dk, ks, where, "dk"), _token_rows(dv, ks, where, "dv")
-    rc = lib.swaa_qk_norm_rope_backward(qp, kp, qn, kn, _dense(dq_out, qs, bf, where, "dq_out"), _dense(dk_out, ks, bf, where, "dk_out"),
-                                        _dense(dv_out, ks, bf, where, "dv_out"), qw, kw, float(eps), f, rot, int(bool(interleaved)),
-                                        _dense(positions, (T,), torch.int32, where, "positions"), T, Hq, Hkv, D, dqp, dkp, dvp, dqn, dkn, dvn,
-                                        _dense(dq_weight, (D,), f32, where, "dq_weight"), _dense(dk_weight, (D,), f32, where, "dk_weight"),
-                                        _dev_ptr(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(),
+    (qp, qn), (kp, kn) = _token_rows(q, qs, where, "q", dev), _token_rows(k, ks, where, "k", dev)
+    (dqp, dqn), (dkp, dkn), (dvp, dvn) = _token_rows(dq, qs, where, "dq", dev), _token_rows(dk, ks, where, "dk", dev), \
+        _token_rows(dv, ks, where, "dv", dev)
+    rc = lib.swaa_qk_norm_rope_backward(qp, kp, qn, kn, _dense(dq_out, qs, bf, where, "dq_out", dev), _dense(dk_out, ks, bf, where, "dk_out", dev),
+                                        _dense(dv_out, ks, bf, where, "dv_out", dev), qw, kw, float(eps), f, rot, int(bool(interleaved)),
+                                        _dense(positions, (T,), torch.int32, where, "positions", dev), T, Hq, Hkv, D, dqp, dkp, dvp, dqn, dkn, dvn,
+                                        _dense(dq_weight, (D,), f32, where, "dq_weight", dev), _dense(dk_weight, (D,), f32, where, "dk_weight", dev),
+                                        _dense(workspace, None, torch.uint8, where, "workspace", dev), 0 if workspace is None else workspace.numel(),
                                         _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
 
 def _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps, interleaved):
-    """The arguments that swaa_cache_append and swaa_cache_append_paged pass on first, the address of q_out, and their sizes."""
-    T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
+    """The arguments that swaa_cache_append and swaa_cache_append_paged pass on first, the address of q_out, the device, and their sizes."""
+    dev, T, Hq, Hkv, D, qw, kw, f, rot = _rope_args(where, q, k, q_weight, k_weight, inv_freq)
     if v is None:
         raise ValueError(f"{where}: v is needed")
     B = seqlens_k.numel()
     i32, qs, ks = torch.int32, (T, Hq, D), (T, Hkv, D)
     if cu_seqlens_q.numel() != B + 1:
         raise ValueError(f"{where}: cu_seqlens_q must be [B + 1] and seqlens_k [B]")
-    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q"), _token_rows(k, ks, where, "k"), _token_rows(v, ks, where, "v")
-    return (qp, kp, vp, qn, kn, vn, qw, kw, float(eps), f, rot, int(bool(interleaved)), _dense(positions, (T,), i32, where, "positions"),
-            _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k")), \
-        _dense(q_out, qs, torch.bfloat16, where, "q_out"), B, T, Hq, Hkv, D
+    (qp, qn), (kp, kn), (vp, vn) = _token_rows(q, qs, where, "q", dev), _token_rows(k, ks, where, "k", dev), _token_rows(v, ks, where, "v", dev)
+    return (qp, kp, vp, qn, kn, vn, qw, kw, float(eps), f, rot, int(bool(interleaved)), _dense(positions, (T,), i32, where, "positions", dev),
+            _dense(cu_seqlens_q, None, i32, where, "cu_seqlens_q", dev), _dense(seqlens_k, None, i32, where, "seqlens_k", dev)), \
+        _dense(q_out, qs, torch.bfloat16, where, "q_out", dev), dev, B, T, Hq, Hkv, D
 
 
 def swaa_cache_append(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, kcache, vcache, positions=None, window: int = 0,
@@ -717,12 +728,12 @@ def swaa_cache_append(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqle
     positions int32 [Tq] or None (the entry's index); window > 0: the caches are rings as in trimmed_cache_slot."""
     lib = _lib or load_library()
     where = "swaa_cache_append"
-    args, qo, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
+    args, qo, dev, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
                                               interleaved)
     bf, Lmax = torch.bfloat16, kcache.shape[1]
     shape = (B, Lmax, Hkv, D)
-    rc = lib.swaa_cache_append(*args, B, T, Lmax, Hq, Hkv, D, int(window), int(n_sink), qo, _dense(kcache, shape, bf, where, "kcache"),
-                               _dense(vcache, shape, bf, where, "vcache"), _stream_ptr(stream))
+    rc = lib.swaa_cache_append(*args, B, T, Lmax, Hq, Hkv, D, int(window), int(n_sink), qo, _dense(kcache, shape, bf, where, "kcache", dev),
+                               _dense(vcache, shape, bf, where, "vcache", dev), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -733,7 +744,7 @@ def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q,
     block_table int32 [B,max_blocks]."""
     lib = _lib or load_library()
     where = "swaa_cache_append_paged"
-    args, qo, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
+    args, qo, dev, B, T, Hq, Hkv, D = _append_args(where, q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q, seqlens_k, q_out, positions, eps,
                                               interleaved)
     bf = torch.bfloat16
     num_pages, page_size = kpages.shape[:2]
@@ -741,8 +752,10 @@ def swaa_cache_append_paged(q, k, v, q_weight, k_weight, inv_freq, cu_seqlens_q,
     rows, max_blocks = _table_shape(block_table)
     if rows != B:
         raise ValueError(f"{where}: block_table must be [B, max_blocks]")
-    rc = lib.swaa_cache_append_paged(*args, _dev_ptr(block_table, torch.int32, "block_table"), B, T, max_blocks, num_pages, page_size, Hq, Hkv, D,
-                                     qo, _dense(kpages, shape, bf, where, "kpages"), _dense(vpages, shape, bf, where, "vpages"), _stream_ptr(stream))
+    rc = lib.swaa_cache_append_paged(*args,
+                                     _dense(block_table, None, torch.int32, where, "block_table", dev), B, T, max_blocks, num_pages, page_size, Hq, Hkv, D,
+                                     qo, _dense(kpages, shape, bf, where, "kpages", dev),
+                                     _dense(vpages, shape, bf, where, "vpages", dev), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -776,7 +789,7 @@ def swaa_key_weights(q, k, lse, weights_in, weights_out, cu_seqlens_q, cu_seqlen
     weights_out, or None for zeros; entries of the call's own tokens start from 0); workspace: uint8 of key_weights_workspace_size(...)."""
     lib = load_library()
     where = "swaa_key_weights"
-    _on_current_device(q, where)
+    dev = _current_device(q, where)
     Tq, Hq, D = q.shape
     Tk, Hkv = k.shape[0], k.shape[1]
     B = cu_seqlens_q.numel() - 1
@@ -785,10 +798,12 @@ def swaa_key_weights(q, k, lse, weights_in, weights_out, cu_seqlens_q, cu_seqlen
     _shaped(lse, (Hq, Tq), where, "lse")
     rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
-    rc = lib.swaa_key_weights(_dev_ptr(q, bf, "q"), _dev_ptr(k, bf, "k"), _dev_ptr(lse, f32, "lse"), _dev_ptr(weights_in, f32, "weights_in"),
-                              _dev_ptr(weights_out, f32, "weights_out"), _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"),
-                              _dev_ptr(cu_seqlens_k, i32, "cu_seqlens_k"), B, Tq, Tk, int(max_seqlen_q), int(max_seqlen_k), rows, Hq, Hkv, D,
-                              int(window), int(n_sink), int(bool(is_full)), float(scale), int(last), _dev_ptr(workspace, torch.uint8, "workspace"),
+    rc = lib.swaa_key_weights(_dense(q, None, bf, where, "q", dev), _dense(k, None, bf, where, "k", dev), _dense(lse, None, f32, where, "lse", dev),
+                              _dense(weights_in, None, f32, where, "weights_in", dev),
+                              _dense(weights_out, None, f32, where, "weights_out", dev), _dense(cu_seqlens_q, None, i32, where, "cu_seqlens_q", dev),
+                              _dense(cu_seqlens_k, None, i32, where, "cu_seqlens_k", dev), B, Tq, Tk, int(max_seqlen_q), int(max_seqlen_k), rows, Hq, Hkv, D,
+                              int(window), int(n_sink), int(bool(is_full)), float(scale), int(last),
+                              _dense(workspace, None, torch.uint8, where, "workspace", dev),
                               workspace.numel(), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
@@ -800,7 +815,7 @@ def swaa_key_weights_paged(q, kpages, lse, weights_in, weights_out, cu_seqlens_q
     block_table int32 [B,max_blocks], seqlens_k int32 [B] of them."""
     lib = load_library()
     where = "swaa_key_weights_paged"
-    _on_current_device(q, where)
+    dev = _current_device(q, where)
     Tq, Hq, D = q.shape
     num_pages, page_size, Hkv, _ = kpages.shape
     B = cu_seqlens_q.numel() - 1
@@ -809,12 +824,15 @@ def swaa_key_weights_paged(q, kpages, lse, weights_in, weights_out, cu_seqlens_q
     _shaped(lse, (Hq, Tq), where, "lse")
     rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
     bf, f32, i32 = torch.bfloat16, torch.float32, torch.int32
-    rc = lib.swaa_key_weights_paged(_dev_ptr(q, bf, "q"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(lse, f32, "lse"),
-                                    _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
-                                    _dev_ptr(cu_seqlens_q, i32, "cu_seqlens_q"), _dev_ptr(seqlens_k, i32, "seqlens_k"),
-                                    _dev_ptr(block_table, i32, "block_table"), B, Tq, int(max_seqlen_q), block_table.shape[1], num_pages, page_size,
+    rc = lib.swaa_key_weights_paged(_dense(q, None, bf, where, "q", dev), _dense(kpages, None, bf, where, "kpages", dev),
+                                    _dense(lse, None, f32, where, "lse", dev),
+                                    _dense(weights_in, None, f32, where, "weights_in", dev),
+                                    _dense(weights_out, None, f32, where, "weights_out", dev),
+                                    _dense(cu_seqlens_q, None, i32, where, "cu_seqlens_q", dev),
+                                    _dense(seqlens_k, None, i32, where, "seqlens_k", dev),
+                                    _dense(block_table, None, i32, where, "block_table", dev), B, Tq, int(max_seqlen_q), block_table.shape[1], num_pages, page_size,
                                     rows, Hq, Hkv, D, int(window), int(n_sink), int(bool(is_full)), float(scale), int(last),
-                                    _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(), _stream_ptr(stream))
+                                    _dense(workspace, None, torch.uint8, where, "workspace", dev), workspace.numel(), _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
 
@@ -832,17 +850,18 @@ def swaa_decode_weighted(q, kcache, vcache, out, weights_in, weights_out, seqlen
     zeros; the new token's own entry starts from 0); workspace: uint8 of decode_weighted_workspace_size(...) bytes."""
     lib = load_library()
     where = "swaa_decode_weighted"
-    _on_current_device(q, where)
+    dev = _current_device(q, where)
     B, Hq, D = q.shape
     _, Lmax, Hkv, _ = kcache.shape
     if kcache.shape != (B, Lmax, Hkv, D) or vcache.shape != (B, Lmax, Hkv, D) or out.shape != (B, Hq, D) or seqlens.numel() != B:
         raise ValueError("swaa_decode_weighted: inconsistent tensor shapes")
     rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
     bf, f32 = torch.bfloat16, torch.float32
-    rc = lib.swaa_decode_weighted(_dev_ptr(q, bf, "q"), _dev_ptr(kcache, bf, "kcache"), _dev_ptr(vcache, bf, "vcache"), _dev_ptr(out, bf, "out"),
-                                  _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
-                                  _dev_ptr(seqlens, torch.int32, "seqlens"), B, Lmax, rows, Hq, Hkv, D, int(window), int(n_sink),
-                                  int(bool(is_full)), float(scale), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+    rc = lib.swaa_decode_weighted(_dense(q, None, bf, where, "q", dev), _dense(kcache, None, bf, where, "kcache", dev),
+                                  _dense(vcache, None, bf, where, "vcache", dev), _dense(out, None, bf, where, "out", dev),
+                                  _dense(weights_in, None, f32, where, "weights_in", dev), _dense(weights_out, None, f32, where, "weights_out", dev),
+                                  _dense(seqlens, None, torch.int32, where, "seqlens", dev), B, Lmax, rows, Hq, Hkv, D, int(window), int(n_sink),
+                                  int(bool(is_full)), float(scale), _dense(workspace, None, torch.uint8, where, "workspace", dev), workspace.numel(),
                                   _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
@@ -853,7 +872,7 @@ def swaa_decode_weighted_paged(q, kpages, vpages, out, weights_in, weights_out, 
     """Forwards to C swaa_decode_weighted_paged: swaa_decode_paged with the weights of swaa_decode_weighted."""
     lib = load_library()
     where = "swaa_decode_weighted_paged"
-    _on_current_device(q, where)
+    dev = _current_device(q, where)
     B, Hq, D = q.shape
     num_pages, page_size, Hkv, _ = kpages.shape
     if vpages.shape != kpages.shape or kpages.shape[3] != D or out.shape != (B, Hq, D):
@@ -862,11 +881,15 @@ def swaa_decode_weighted_paged(q, kpages, vpages, out, weights_in, weights_out, 
         raise ValueError("swaa_decode_weighted_paged: block_table must be [B, max_blocks] and seqlens [B]")
     rows = _weights_rows(where, weights_in, weights_out, B, Hkv)
     bf, f32 = torch.bfloat16, torch.float32
-    rc = lib.swaa_decode_weighted_paged(_dev_ptr(q, bf, "q"), _dev_ptr(kpages, bf, "kpages"), _dev_ptr(vpages, bf, "vpages"), _dev_ptr(out, bf, "out"),
-                                        _dev_ptr(weights_in, f32, "weights_in"), _dev_ptr(weights_out, f32, "weights_out"),
-                                        _dev_ptr(block_table, torch.int32, "block_table"), _dev_ptr(seqlens, torch.int32, "seqlens"), B,
+    rc = lib.swaa_decode_weighted_paged(_dense(q, None, bf, where, "q", dev), _dense(kpages, None, bf, where, "kpages", dev),
+                                        _dense(vpages, None, bf, where, "vpages", dev), _dense(out, None, bf, where, "out", dev),
+                                        _dense(weights_in, None, f32, where, "weights_in", dev),
+                                        _dense(weights_out, None, f32, where, "weights_out", dev),
+                                        _dense(block_table, None, torch.int32, where, "block_table", dev),
+                                        _dense(seqlens, None, torch.int32, where, "seqlens", dev), B,
                                         block_table.shape[1], num_pages, page_size, rows, Hq, Hkv, D, int(window), int(n_sink),
-                                        int(bool(is_full)), float(scale), _dev_ptr(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                        int(bool(is_full)), float(scale),
+                                        _dense(workspace, None, torch.uint8, where, "workspace", dev), workspace.numel(),
                                         _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)
@@ -874,16 +897,18 @@ def swaa_decode_weighted_paged(q, kpages, vpages, out, weights_in, weights_out, 
 
 def _evict_args(where, kcache, vcache, weights, seqlens, budget, kcache_out, vcache_out, weights_out, kept, seqlens_out):
     """Sizes of an eviction's arguments and the addresses of those that both forms take."""
-    _on_current_device(kcache, where)
+    dev = _current_device(kcache, where)
     B, (n, rows, Hkv, D), (n_out, rows_out, _, _) = seqlens.numel(), kcache.shape, kcache_out.shape
     w_rows, wo_rows = weights.shape[-1], weights_out.shape[-1]
     bf, f32, i32, shape, shape_out = torch.bfloat16, torch.float32, torch.int32, (n, rows, Hkv, D), (n_out, rows_out, Hkv, D)
-    inputs = (_dense(kcache, shape, bf, where, "kcache"), _dense(vcache, shape, bf, where, "vcache"), _dense(weights, (B, Hkv, w_rows), f32, where, "weights"),
-              _dev_ptr(seqlens, i32, "seqlens"))
-    caches = _dense(kcache_out, shape_out, bf, where, "kcache_out"), _dense(vcache_out, shape_out, bf, where, "vcache_out")
-    outputs = (_dense(weights_out, (B, Hkv, wo_rows), f32, where, "weights_out"), wo_rows, _dense(kept, (B, Hkv, budget), i32, where, "kept"),
-               _dense(seqlens_out, (B,), i32, where, "seqlens_out"))
-    return B, Hkv, D, w_rows, shape, shape_out, inputs, caches, outputs
+    inputs = (_dense(kcache, shape, bf, where, "kcache", dev), _dense(vcache, shape, bf, where, "vcache", dev),
+              _dense(weights, (B, Hkv, w_rows), f32, where, "weights", dev),
+              _dense(seqlens, None, i32, where, "seqlens", dev))
+    caches = _dense(kcache_out, shape_out, bf, where, "kcache_out", dev), _dense(vcache_out, shape_out, bf, where, "vcache_out", dev)
+    outputs = (_dense(weights_out, (B, Hkv, wo_rows), f32, where, "weights_out", dev), wo_rows,
+               _dense(kept, (B, Hkv, budget), i32, where, "kept", dev),
+               _dense(seqlens_out, (B,), i32, where, "seqlens_out", dev))
+    return dev, B, Hkv, D, w_rows, shape, shape_out, inputs, caches, outputs
 
 
 def swaa_cache_evict(kcache, vcache, weights, seqlens, budget: int, n_sink: int, recent: int, kcache_out, vcache_out, weights_out, kept,
@@ -893,8 +918,8 @@ def swaa_cache_evict(kcache, vcache, weights, seqlens, budget: int, n_sink: int,
     [B,>=budget,Hkv,D] bf16, weights_out f32 [B,Hkv,>=budget]; kept int32 [B,Hkv,budget]: their old index; seqlens_out int32 [B]."""
     lib = _lib or load_library()
     where = "swaa_cache_evict"
-    B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(where, kcache, vcache, weights, seqlens, int(budget), kcache_out, vcache_out,
-                                                                             weights_out, kept, seqlens_out)
+    dev, B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(
+        where, kcache, vcache, weights, seqlens, int(budget), kcache_out, vcache_out, weights_out, kept, seqlens_out)
     if shape[0] != B or shape_out[0] != B:
         raise ValueError(f"{where}: caches must be [B, entries, Hkv, D]")
     rc = lib.swaa_cache_evict(*inputs, B, shape[1], rows, Hkv, D, int(budget), int(n_sink), int(recent), *caches, shape_out[1], *outputs,
@@ -909,14 +934,16 @@ def swaa_cache_evict_paged(kpages, vpages, weights, seqlens, block_table, budget
     [B,max_blocks] into pages behind block_table_out (of the same pool or another; none that the call reads)."""
     lib = _lib or load_library()
     where = "swaa_cache_evict_paged"
-    B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(where, kpages, vpages, weights, seqlens, int(budget), kpages_out, vpages_out,
-                                                                             weights_out, kept, seqlens_out)
+    dev, B, Hkv, D, rows, shape, shape_out, inputs, caches, outputs = _evict_args(
+        where, kpages, vpages, weights, seqlens, int(budget), kpages_out, vpages_out, weights_out, kept, seqlens_out)
     (n, blocks), (n_out, blocks_out) = _table_shape(block_table), _table_shape(block_table_out)
     if n != B or n_out != B:
         raise ValueError(f"{where}: block_table and block_table_out must be [B, max_blocks]")
     i32 = torch.int32
-    rc = lib.swaa_cache_evict_paged(*inputs, _dev_ptr(block_table, i32, "block_table"), B, blocks, shape[0], shape[1], rows, Hkv, D, int(budget),
-                                    int(n_sink), int(recent), *caches, _dev_ptr(block_table_out, i32, "block_table_out"), blocks_out, shape_out[0],
+    rc = lib.swaa_cache_evict_paged(*inputs,
+                                    _dense(block_table, None, i32, where, "block_table", dev), B, blocks, shape[0], shape[1], rows, Hkv, D, int(budget),
+                                    int(n_sink), int(recent), *caches,
+                                    _dense(block_table_out, None, i32, where, "block_table_out", dev), blocks_out, shape_out[0],
                                     shape_out[1], *outputs, _stream_ptr(stream))
     if rc != SWAA_OK:
         raise SwaaError(rc, where)

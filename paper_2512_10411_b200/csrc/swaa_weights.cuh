@@ -244,7 +244,8 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             x.m_lo = x.span.lo + chunk * share;
             x.nm = max(min(x.span.hi, x.m_lo + share - 1) - x.m_lo + 1, 0);
         }
-        if (p.cu_k == nullptr && (x.page = key_weights_page(p, b, t * BK)) < 0) x.nm = 0;
+        // (keys that no query sees need no page: what lies before the windows of a long sequence may have been given up)
+        if (p.cu_k == nullptr && x.nm > 0 && (x.page = key_weights_page(p, b, t * BK)) < 0) x.nm = 0;
         return x;
     };
     // What the block found out for key j of tile t: the whole sum, or that of its chunk.

@@ -233,7 +233,24 @@ def test_blocks_of_several_key_tiles(Hq, D, last, mask, paged):
         t[5, 6] = -1
         w_out.fill_(9.0)
         call({**s, "table": t}, None, w_out, mask, last)
-        assert swaa.status_str(swaa.last_device_status()) == "SWAA_ERR_BAD_SEQLENS"
-        assert (w_out[5, :, 768:896] == 9).all()
-        before[5, :, 768:896] = 9.0
+        if mask[2]:
+            assert swaa.status_str(swaa.last_device_status()) == "SWAA_ERR_BAD_SEQLENS"
+            assert (w_out[5, :, 768:896] == 9).all()
+            before[5, :, 768:896] = 9.0
+        else:  # none of the last queries sees so far back, and 768 is past the sinks
+            assert swaa.last_device_status() == 0
         assert torch.equal(w_out, before)
+
+
+def test_pages_that_no_query_sees_may_be_gone():
+    """Pages before the windows of a call (and without sinks) are not looked up: their keys keep what they had."""
+    new, ctx, mask = (70, 9), (1000, 700), (200, 0, False)
+    s = make(new, ctx, 8, 2, 64, 13, paged=True)
+    w_in = torch.rand(2, 2, 1024, device="cuda")
+    want, got = torch.full_like(w_in, 9.0), torch.full_like(w_in, 9.0)
+    call(s, w_in, want, mask)
+    t = s["table"].clone()
+    t[0, :5], t[1, :3] = -1, 10 ** 6  # the first query of sequence 0 is at 930 and sees keys from 731 on, that of sequence 1 from 492 on
+    call({**s, "table": t}, w_in, got, mask)
+    assert swaa.last_device_status() == 0
+    assert torch.equal(got, want) and torch.equal(got[0, :, :640], w_in[0, :, :640])
