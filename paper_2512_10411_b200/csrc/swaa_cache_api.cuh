@@ -466,6 +466,8 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     DeviceInfo info;
     if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
     const int G = Hq / Hkv, rows = last > 0 && last < max_q ? last : max_q;
+    // Up to 64 queries fill half of a step's columns: two heads share it where the group has an even number of them.  The last 64 queries of
+    // eight prompts of 145610 tokens in all, 32 heads of 128, 8 key heads: 191 us with a head a step, 130 with two.
     const int hs = G % 2 == 0 && 2 * rows <= kKeyWeightsRows ? 2 : 1;
     CUtensorMap tq = {}, tk = {};
     if (Tq > 0 && (rc = make_token_major_map(&tq, q, Tq, Hq, D, kKeyWeightsRows / hs, hs)) != SWAA_OK) return rc;
@@ -504,7 +506,8 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     p.sink_tiles = pl.sink_tiles;
     p.sink_chunks = pl.sink_chunks;
     p.heads_per_step = hs;
-    // A block of few steps is mostly set-up: it takes more key tiles while there are several blocks per SM all the same.
+    // A block of few steps is mostly set-up: it takes more key tiles, up to 16 steps, while there are several blocks per SM all the same.  The same
+    // call with 4, 8, 16 and 32 steps: 192, 158, 149 and 150 us (an earlier form of the kernel); one prompt of 32768 tokens 48 throughout.
     const long long steps = std::max(1ll, ((long long)rows + kKeyWeightsRows - 1) / kKeyWeightsRows) * (G / hs);
     p.run = 1;
     while (p.run * steps < kKeyWeightsRunSteps && (long long)B * Hkv * (pl.key_tiles / (2 * p.run)) >= 8ll * info.sm_count) p.run *= 2;

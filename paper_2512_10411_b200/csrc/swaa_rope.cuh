@@ -290,7 +290,7 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
 template <int D, bool kPairs, bool kCache>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams p) {
     using L = RopeLane<D, kPairs>;
-    extern __shared__ __align__(128) uint8_t smem_raw[];
+    extern __shared__ __align__(128) uint8_t rope_smem[];
     __shared__ uint64_t bar_words[kRopeWarps * kRopeStages];
     __shared__ int abort_word;
     if (threadIdx.x == 0) abort_word = 0;
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     float wa[8], wb[8];
     load_weights(w, ln.a0, wa);
     load_weights(w, ln.b0, wb);
-    RopeRing ring(smem_u32(smem_raw), bar_words, &abort_word, (int)threadIdx.x >> 5, lane);
+    RopeRing ring(smem_u32(rope_smem), bar_words, &abort_word, (int)threadIdx.x >> 5, lane);
     uint32_t bytes = 0;  // of a share
 #pragma unroll
     for (int u = 0; u < kRopeRows; ++u)
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
 template <int D, bool kPairs>
 __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const RopeGradParams p) {
     using L = RopeLane<D, kPairs>;
-    extern __shared__ __align__(128) uint8_t smem_raw[];
+    extern __shared__ __align__(128) uint8_t rope_smem[];
     __shared__ float sm_w[kRopeWarps][D];
     __shared__ uint64_t bar_words[kRopeWarps * kRopeStages];
     __shared__ int abort_word;
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const Ro
     load_weights(w, ln.b0, wb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) da[i] = db[i] = 0.f;
-    RopeRing ring(smem_u32(smem_raw), bar_words, &abort_word, wid, lane);
+    RopeRing ring(smem_u32(rope_smem), bar_words, &abort_word, wid, lane);
     uint32_t bytes = 0;  // of a share
 #pragma unroll
     for (int u = 0; u < kRopeBwdRows; ++u)

@@ -15,7 +15,7 @@
 // turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than kKeyWeightsChunk query tiles is cut into
 // chunks for blocks of their own (every tile under full attention, the sinks under a window); the chunks' sums are added in order by
 // a second kernel, so results do not depend on scheduling.  Where few queries count (the last ones of a prompt) a step takes 64 queries
-// of two heads, and a block several tiles of keys one after another, its queries staying where they are.
+// of two heads, and a block several tiles of keys one after another.
 //
 // What bounds it: shared memory and the exponentials, one per visible pair.  A step of 128 x 128 moves through shared memory the operands of its
 // products (512 cycles at D = 128), its queries (256) and four readings of the log-sum-exps (128), and takes 1024 cycles of
@@ -287,8 +287,6 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     static_assert(2 * BR == 256, "tensor memory columns");
-    // Where every tile of the run meets the same few queries, they are loaded once and stay.
-    const bool resident = p.run > 1 && s.nq <= BR / hs && head_steps <= NQ;
     bool ok = true;
 
     if (warp == 8) {
@@ -312,18 +310,16 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int h = 0; h < head_steps && ok; ++h)
                 for (int m = 0; m < x.nm; ++m) {
                     const int head = hk * p.G + h * hs, i0 = (x.m_lo + m) * BR;  // from pos0
-                    if (!resident || tiles == 1) {
-                        const int st = loads % NQ;
-                        if (loads >= NQ) ok = warp_wait(bar(BAR_QE + st), (uint32_t)(loads / NQ - 1) & 1u, abort_flag);
-                        if (!ok) break;
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(bar(BAR_QF + st), (uint32_t)L::kTileBytes);
+                    const int st = steps % NQ;
+                    if (steps >= NQ) ok = warp_wait(bar(BAR_QE + st), (uint32_t)(steps / NQ - 1) & 1u, abort_flag);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx(bar(BAR_QF + st), (uint32_t)L::kTileBytes);
 #pragma unroll
-                            for (int pn = 0; pn < L::kPanels; ++pn)
-                                tma_load_3d(sRing + (uint32_t)(st * L::kTileBytes + pn * L::kPanelBytes), &tm_q, pn * 64, head, first + i0, bar(BAR_QF + st));
-                        }
-                        ++loads;
+                        for (int pn = 0; pn < L::kPanels; ++pn)
+                            tma_load_3d(sRing + (uint32_t)(st * L::kTileBytes + pn * L::kPanelBytes), &tm_q, pn * 64, head, first + i0, bar(BAR_QF + st));
                     }
+                    ++loads;
                     const int sl = steps % NL;
                     if (steps >= NL) ok = warp_wait(bar(BAR_LE + sl), (uint32_t)(steps / NL - 1) & 1u, abort_flag);
                     if (!ok) break;
@@ -360,8 +356,8 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             ok = warp_wait(bar(BAR_KF), (uint32_t)tiles & 1u, abort_flag);
             ++tiles;
             for (int i = 0; i < n_steps && ok; ++i, ++n) {
-                const int ld = resident ? i : n, st = ld % NQ, buf = n & 1;
-                ok = warp_wait(bar(BAR_QF + st), (uint32_t)(ld / NQ) & 1u, abort_flag) &&
+                const int st = n % NQ, buf = n & 1;
+                ok = warp_wait(bar(BAR_QF + st), (uint32_t)(n / NQ) & 1u, abort_flag) &&
                      warp_wait(bar(BAR_SE + buf), ((uint32_t)(n >> 1) & 1u) ^ 1u, abort_flag);  // the buffers start out free
                 if (!ok) break;
                 tc_fence_after();
@@ -373,7 +369,7 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                         mma_ss_lh(d, k_a + o, q + o, hi, kIdS, kk > 0 ? 1u : 0u);
                     }
                     tc_commit(bar(BAR_SF + buf));
-                    if (!resident) tc_commit(bar(BAR_QE + st));
+                    tc_commit(bar(BAR_QE + st));
                     if (i == n_steps - 1) tc_commit(bar(BAR_KE));
                 }
             }
