@@ -240,3 +240,121 @@ def test_training_step_through_norm_and_rotation():
         # q, k, v, P, dS, dq, dk and the result are rounded to bf16 on the way, half a step each of what they are: at most 8 of them
         # in the 2-norm, and along a random direction of unit variance an error vector of norm e shows with standard deviation e
         assert np.max(np.abs(errs)) <= 4 * 8 * ref.HALF_BF16 * np.mean(size), (what, errs, size)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of more than 2^31 elements: append, decode with weights, eviction, pages and token strides at its far end."""
+    Hkv, D, pages = 8, 128, 17200
+    L = pages * 128
+    assert L * Hkv * D > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(6)
+    kc, vc = (torch.zeros(1, L, Hkv, D, dtype=BF, device="cuda") for _ in range(2))
+    f = (1e4 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)).float().cuda()
+    # append: the last entry, nothing else
+    qkv = torch.randn(1, 3 * Hkv, D, generator=g, device="cuda").to(BF)
+    q1, k1, v1 = qkv.split((Hkv, Hkv, Hkv), 1)
+    q = torch.empty(1, Hkv, D, dtype=BF, device="cuda")
+    swaa.swaa_cache_append(q1, k1, v1, None, None, f, int32([0, 1]), int32([L]), q, kc, vc)
+    want, bound = ref.qk_rope(f64(k1), None, EPS, np.array([L - 1]), f64(f), False)
+    assert (np.abs(f64(kc[:, L - 1]) - want) <= bound).all() and torch.equal(vc[:, L - 1], v1)
+    assert not kc[0, :L - 1].any() and not vc[0, :L - 1].any()
+    # decode with weights: every other key scores 0
+    w = torch.full((1, Hkv, L), float("nan"), device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(swaa.decode_weighted_workspace_size(1, Hkv, Hkv, D, L, 1, 0, True), dtype=torch.uint8, device="cuda")
+    swaa.swaa_decode_weighted(q, kc, vc, out, None, w, int32([L]), 1, 0, True, ws)
+    assert swaa.last_device_status() == 0
+    x = np.einsum("hd,hd->h", f64(q[0]), f64(kc[0, L - 1])) * D ** -0.5
+    rest = 1 / (L - 1 + np.exp(x))
+    # fp32 row sums of 2.2 million terms, in runs of a block's keys: 1e-4 is above the half steps of the longest run (15000 keys)
+    np.testing.assert_allclose(f64(w[0, :, L - 1]), np.exp(x) * rest, rtol=2e-3)
+    np.testing.assert_allclose(f64(w[0, :, [0, 1, L // 2, L - 2]]), np.repeat(rest[:, None], 4, 1), rtol=2e-3)
+    np.testing.assert_allclose(f64(w[0].double().sum(-1)), 1.0, rtol=2e-3)
+    # eviction: entries far apart
+    w.zero_()
+    at = [5, 1_000_000, L - 70_000, L - 3]
+    for i, j in enumerate(at):
+        w[0, :, j] = 1.0 + i
+        kc[0, j], vc[0, j] = torch.randn(Hkv, D, generator=g, device="cuda").to(BF), torch.randn(Hkv, D, generator=g, device="cuda").to(BF)
+    N = 8  # two sinks, two recent entries, those four
+    ko, vo, wo = torch.empty(1, N, Hkv, D, dtype=BF, device="cuda"), torch.empty(1, N, Hkv, D, dtype=BF, device="cuda"), torch.empty(1, Hkv, N, device="cuda")
+    kept, n_out = torch.empty(1, Hkv, N, dtype=torch.int32, device="cuda"), torch.empty(1, dtype=torch.int32, device="cuda")
+    swaa.swaa_cache_evict(kc, vc, w, int32([L]), N, 2, 2, ko, vo, wo, kept, n_out)
+    assert swaa.last_device_status() == 0
+    keep = sorted([0, 1, L - 2, L - 1] + at)
+    assert kept.tolist() == [[keep] * Hkv] and torch.equal(ko[0], kc[0, keep]) and torch.equal(vo[0], vc[0, keep])
+    # pages at both ends of the pool, against the same keys packed
+    kp, table = kc.view(pages, 128, Hkv, D), int32([[pages - 1, pages - 2, 0]])
+    kp[[pages - 1, pages - 2, 0]] = torch.randn(3, 128, Hkv, D, generator=g, device="cuda").to(BF)
+    keys = torch.cat([kp[pages - 1], kp[pages - 2], kp[0]])[:300].contiguous()
+    qq, lse = torch.randn(300, 2 * Hkv, D, generator=g, device="cuda").to(BF), 3 + torch.randn(2 * Hkv, 300, generator=g, device="cuda")
+    got = [torch.zeros(1, Hkv, 384, device="cuda") for _ in range(2)]
+    ws = torch.empty(swaa.key_weights_workspace_size(1, 300, 384, 2 * Hkv, Hkv, 1, 0, True), dtype=torch.uint8, device="cuda")
+    swaa.swaa_key_weights_paged(qq, kp, lse, None, got[0], int32([0, 300]), int32([300]), table, 300, 1, 0, True, ws)
+    swaa.swaa_key_weights(qq, keys, lse, None, got[1], int32([0, 300]), int32([0, 300]), 300, 300, 1, 0, True, ws)
+    assert swaa.last_device_status() == 0 and torch.equal(*got) and got[0].any()
+    # tokens more than 2^30 elements apart
+    far = kc.view(-1).as_strided((3, Hkv, D), (1_100_000_000, D, 1))
+    far.copy_(torch.randn(3, Hkv, D, generator=g, device="cuda"))
+    res = [torch.empty(3, Hkv, D, dtype=BF, device="cuda") for _ in range(4)]
+    pos = int32([1, 2, 3])
+    swaa.swaa_qk_norm_rope(far, far, None, None, None, f, pos, res[0], res[1], None)
+    near = far.contiguous()
+    swaa.swaa_qk_norm_rope(near, near, None, None, None, f, pos, res[2], res[3], None)
+    assert torch.equal(res[0], res[2]) and torch.equal(res[1], res[3])
+    swaa.swaa_qk_norm_rope_backward(None, None, near, near, None, None, None, f, pos, far, res[1], None, None, None, None)
+    swaa.swaa_qk_norm_rope_backward(None, None, near, near, None, None, None, f, pos, res[2], res[3], None, None, None, None)
+    assert torch.equal(far, res[2]) and torch.equal(res[1], res[3]) and swaa.last_device_status() == 0
+
+
+def test_calls_at_once_on_three_streams():
+    """Prefill, key weights, decode with weights, eviction and norm + rotation, overlapping on three streams, give what they give one
+    after another."""
+    layer, n = Layer(7), 4000
+    qkv = layer.project(n)
+    q, k, v, _, _ = prefill(layer, qkv, (n,), (500, 4, False))
+    cu, lse = int32([0, n]), torch.empty(HQ, n, device="cuda")
+    swaa.swaa_prefill(q, k, v, torch.empty_like(q), cu, n, 500, 4, False, lse=lse)
+    kc, vc, lens = k[None].contiguous(), v[None].contiguous(), int32([n])
+    w_in = torch.rand(1, HKV, n, generator=layer.g, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+
+    def work(i):
+        """The calls of stream i with buffers of their own: (run, outputs)."""
+        out = [torch.zeros_like(q) for _ in range(2)] + [torch.zeros(1, HKV, n, device="cuda") for _ in range(2)]
+        ev = [torch.zeros(1, 300, HKV, D, dtype=BF, device="cuda") for _ in range(2)] + [torch.zeros(1, HKV, 300, device="cuda"), torch.zeros(1, HKV, 300, dtype=torch.int32, device="cuda"),
+                                                                                         torch.zeros(1, dtype=torch.int32, device="cuda")]
+        ro = [torch.zeros_like(x) for x in (q, k, v)]
+        ws = [torch.empty(s, dtype=torch.uint8, device="cuda") for s in (swaa.key_weights_workspace_size(1, n, n, HQ, HKV, 500, 4, False),
+                                                                         swaa.decode_weighted_workspace_size(1, HQ, HKV, D, n, 1, 0, True))]
+        dec = torch.zeros(1, HQ, D, dtype=BF, device="cuda")
+
+        def run(stream):
+            for step in range(3):
+                for op in range(5):
+                    what = (op + i) % 5  # every stream in another order
+                    if what == 0:
+                        swaa.swaa_prefill(q, k, v, out[0], cu, n, 500, 4, False, stream=stream)
+                    elif what == 1:
+                        swaa.swaa_key_weights(q, k, lse, None, out[2], cu, cu, n, n, 500, 4, False, ws[0], stream=stream)
+                    elif what == 2:
+                        swaa.swaa_decode_weighted(q[-1:], kc, vc, dec, w_in, out[3], lens, 1, 0, True, ws[1], stream=stream)
+                    elif what == 3:
+                        swaa.swaa_cache_evict(kc, vc, w_in, lens, 300, 4, 50, *ev, stream=stream)
+                    else:
+                        swaa.swaa_qk_norm_rope(*split(qkv), layer.qw, layer.kw, layer.f, pos, *ro, stream=stream)
+
+        return run, [*out, *ev, *ro, dec]
+
+    run, want = work(0)
+    run(None)
+    assert swaa.last_device_status() == 0
+    jobs = [(torch.cuda.Stream(), *work(i)) for i in range(3)]
+    torch.cuda.synchronize()
+    for stream, run, _ in jobs:
+        run(stream)
+    torch.cuda.synchronize()
+    assert swaa.last_device_status() == 0
+    for _, _, got in jobs:
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
