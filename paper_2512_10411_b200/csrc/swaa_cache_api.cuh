@@ -155,13 +155,13 @@ extern "C" int swaa_qk_norm_rope_backward(const void* q, const void* k, long lon
     if (!aligned16(q) || !aligned16(k) || !aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dv_out) || !aligned16(dq) || !aligned16(dk) ||
         !aligned16(dv) || !aligned4(positions))
         return SWAA_ERR_INVALID_ARG;
+    const bool weights = q_weight != nullptr || k_weight != nullptr;
+    if (weights && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)) return SWAA_ERR_WORKSPACE;
     DeviceInfo info;
     if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
     RopeGradParams p = {};
     const unsigned blocks = rope_blocks(T, RopeSplit(Hq, Hkv, D, kRopeBwdRows, dv != nullptr), info.sm_count);
-    const bool weights = q_weight != nullptr || k_weight != nullptr;
-    if (weights && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < (size_t)blocks * 2 * D * sizeof(float)))
-        return SWAA_ERR_WORKSPACE;
+    if (weights && workspace_bytes < (size_t)blocks * 2 * D * sizeof(float)) return SWAA_ERR_WORKSPACE;
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.k = static_cast<const __nv_bfloat16*>(k);
     p.q_stride = q_stride;
@@ -401,17 +401,27 @@ namespace swaa {
 
 // Launch shape and workspace: chunks of the key tiles, [chunks of all tiles | chunks of the tiles that hold sinks].
 struct KeyWeightsPlan {
-    int key_tiles, chunks, sink_tiles, sink_chunks;
+    int heads_per_step, chunk_log, key_tiles, chunks, sink_tiles, sink_chunks;
+    long long steps;  // query tiles of a sequence times groups of heads
     size_t off_sink, bytes;
 };
-static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int Hkv, int window, int n_sink, bool full, int last) {
+static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int G, int Hkv, int window, int n_sink, bool full, int last, int sms) {
     KeyWeightsPlan pl;
     const long long rows = last > 0 && last < max_q ? last : max_q;
+    // Up to 64 queries fill half of a step's columns: two heads share it where the group has an even number of them.  The last 64 queries of
+    // eight prompts of 145610 tokens in all, 32 heads of 128, 8 key heads: 191 us with a head a step, 130 with two.
+    pl.heads_per_step = G % 2 == 0 && 2 * rows <= kKeyWeightsRows ? 2 : 1;
     const long long most = (rows + kKeyWeightsRows - 1) / kKeyWeightsRows;  // query tiles of a sequence
+    pl.steps = std::max(1ll, most) * (G / pl.heads_per_step);
     // a key tile meets the queries of `window + 127` positions, which start anywhere in a tile
     const long long band = full ? most : std::min(most, ((long long)window + kKeyWeightsKeys - 1) / kKeyWeightsRows + 2);
-    auto chunks = [](long long tiles) { return (int)std::max(1ll, (tiles + kKeyWeightsChunk - 1) / kKeyWeightsChunk); };
     pl.key_tiles = (int)(((long long)max_k + kKeyWeightsKeys - 1) / kKeyWeightsKeys);
+    auto chunks = [&](long long tiles) { return (int)std::max(1ll, (tiles + (1ll << pl.chunk_log) - 1) >> pl.chunk_log); };
+    // Calls of few key tiles are cut finer, down to 8 steps a block, until there are two blocks per SM.  Window 2048, us uncut and cut: 1024 tokens,
+    // 32 + 8 heads of 128 32.2 and 20.8; 2048 tokens, 28 + 4 heads 94.4 and 44.5; 4096 tokens, window 512 92.8 and 49.5; 500 and 300 tokens 19.9
+    // and 15.6; 8192 tokens, 4 + 2 heads 51.6 and 38.  Until there are four or eight: the same within 4 %.
+    pl.chunk_log = kKeyWeightsChunkLog;
+    while (pl.chunk_log > 0 && (G / pl.heads_per_step) << pl.chunk_log >= 16 && (long long)B * Hkv * pl.key_tiles * chunks(band) < 2ll * sms) --pl.chunk_log;
     pl.chunks = chunks(band);
     pl.sink_chunks = full ? 1 : chunks(most);
     pl.sink_tiles = pl.sink_chunks > pl.chunks ? (int)std::min<long long>(((long long)n_sink + kKeyWeightsKeys - 1) / kKeyWeightsKeys, pl.key_tiles) : 0;
@@ -461,14 +471,13 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
         return SWAA_ERR_INVALID_ARG;
     const size_t bytes = (size_t)B * Hkv * weights_rows * sizeof(float);
     if (weights_in && weights_in != weights_out && overlap(weights_in, bytes, weights_out, bytes)) return SWAA_ERR_INVALID_ARG;
-    const KeyWeightsPlan pl = key_weights_plan(B, max_q, max_k, Hkv, window, n_sink, is_full != 0, last);
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < pl.bytes) return SWAA_ERR_WORKSPACE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SWAA_ERR_WORKSPACE;
     DeviceInfo info;
     if ((rc = current_sm100(&info)) != SWAA_OK) return rc;
-    const int G = Hq / Hkv, rows = last > 0 && last < max_q ? last : max_q;
-    // Up to 64 queries fill half of a step's columns: two heads share it where the group has an even number of them.  The last 64 queries of
-    // eight prompts of 145610 tokens in all, 32 heads of 128, 8 key heads: 191 us with a head a step, 130 with two.
-    const int hs = G % 2 == 0 && 2 * rows <= kKeyWeightsRows ? 2 : 1;
+    const int G = Hq / Hkv;
+    const KeyWeightsPlan pl = key_weights_plan(B, max_q, max_k, G, Hkv, window, n_sink, is_full != 0, last, info.sm_count);
+    if (workspace_bytes < pl.bytes) return SWAA_ERR_WORKSPACE;
+    const int hs = pl.heads_per_step;
     CUtensorMap tq = {}, tk = {};
     if (Tq > 0 && (rc = make_token_major_map(&tq, q, Tq, Hq, D, kKeyWeightsRows / hs, hs)) != SWAA_OK) return rc;
     if (Tk > 0) {
@@ -506,11 +515,11 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
     p.sink_tiles = pl.sink_tiles;
     p.sink_chunks = pl.sink_chunks;
     p.heads_per_step = hs;
+    p.chunk_log = pl.chunk_log;
     // A block of few steps is mostly set-up: it takes more key tiles, up to 16 steps, while there are several blocks per SM all the same.  The same
     // call with 4, 8, 16 and 32 steps: 192, 158, 149 and 150 us (an earlier form of the kernel); one prompt of 32768 tokens 48 throughout.
-    const long long steps = std::max(1ll, ((long long)rows + kKeyWeightsRows - 1) / kKeyWeightsRows) * (G / hs);
     p.run = 1;
-    while (p.run * steps < kKeyWeightsRunSteps && (long long)B * Hkv * (pl.key_tiles / (2 * p.run)) >= 8ll * info.sm_count) p.run *= 2;
+    while (pl.chunks == 1 && pl.sink_tiles == 0 && p.run * pl.steps < kKeyWeightsRunSteps && (long long)B * Hkv * (pl.key_tiles / (2 * p.run)) >= 8ll * info.sm_count) p.run *= 2;
     p.part = static_cast<float*>(workspace);
     p.sink_part = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_sink);
     cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
@@ -522,7 +531,9 @@ static int key_weights_impl(const void* q, const void* k, const float* lse, cons
 extern "C" size_t swaa_key_weights_workspace_size(int B, int max_seqlen_q, int max_seqlen_k, int Hq, int Hkv, int window, int n_sink,
                                                   int is_full, int last) {
     if (check_key_weights(B, max_seqlen_q, max_seqlen_k, Hq, Hkv, window, n_sink, is_full, last) != SWAA_OK || B == 0) return 256;
-    return key_weights_plan(B, max_seqlen_q, max_seqlen_k, Hkv, window, n_sink, is_full != 0, last).bytes;
+    DeviceInfo info;
+    if (current_device_info(&info) != SWAA_OK) info.sm_count = 148;
+    return key_weights_plan(B, max_seqlen_q, max_seqlen_k, Hq / Hkv, Hkv, window, n_sink, is_full != 0, last, info.sm_count).bytes;
 }
 
 extern "C" int swaa_key_weights(const void* q, const void* k, const float* lse, const float* weights_in, float* weights_out,

@@ -12,7 +12,7 @@
 // One block owns 128 keys of one (sequence, kv head) and walks the 128-query tiles that see them, for every head of the group:
 //     S^T = K Q^T [128 keys x 128 queries], tcgen05.mma, accumulators in tensor memory
 // so that a key is a tensor-memory lane and the sum over queries stays in its thread.  Two groups of four warps take the steps in
-// turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than kKeyWeightsChunk query tiles is cut into
+// turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than 16 query tiles (fewer in small calls) is cut into
 // chunks for blocks of their own (every tile under full attention, the sinks under a window); the chunks' sums are added in order by
 // a second kernel, so results do not depend on scheduling.  Where few queries count (the last ones of a prompt) a step takes 64 queries
 // of two heads, and a block several tiles of keys one after another.
@@ -92,13 +92,14 @@ struct KeyWeightsParams {
     // chunks: [chunks][B][Hkv][128 key_tiles] sums of all tiles, [sink_chunks][B][Hkv][128 sink_tiles] of the tiles that hold sinks
     int key_tiles, chunks, sink_tiles, sink_chunks;
     int run;                      // key tiles of a block, one after another; above 1 nothing is cut into chunks
+    int chunk_log;                // a tile seen by more than 2^chunk_log query tiles is cut
     int heads_per_step;           // 2: a step takes 64 queries of two heads (at most 64 queries of a sequence count)
     float *part, *sink_part;
 };
 
 constexpr int kKeyWeightsKeys = 128;
 constexpr int kKeyWeightsRows = 128;   // columns of a step: queries, or queries of two heads in turn
-constexpr int kKeyWeightsChunk = 16;   // query tiles of a block
+constexpr int kKeyWeightsChunkLog = 4;  // log2 of the query tiles of a block, less in small calls
 constexpr int kKeyWeightsThreads = 320;  // two groups of four warps, producer, issuer
 constexpr int kKeyWeightsRunSteps = 16;  // steps below which a block takes more key tiles
 constexpr int kKeyWeightsLse = 4;      // steps whose log-sum-exps are in shared memory
@@ -136,7 +137,7 @@ __device__ __forceinline__ KeyWeightsSpan key_weights_span(const KeyWeightsParam
         const long long end = (long long)j0 + kKeyWeightsKeys - 1 + p.window - 1 - s.pos0;  // last query, from pos0, that sees the tile's last key
         t.hi = end < 0 ? -1 : (int)(end / kKeyWeightsRows < t.hi ? end / kKeyWeightsRows : t.hi);
     }
-    t.chunks = t.hi < t.lo ? 0 : (t.hi - t.lo + kKeyWeightsChunk) / kKeyWeightsChunk;
+    t.chunks = t.hi < t.lo ? 0 : ((t.hi - t.lo) >> p.chunk_log) + 1;
     return t;
 }
 // The page of a key tile; the pages are multiples of the tile.  -1: not a page of the pool.
