@@ -416,18 +416,31 @@ static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int G, int H
     // a key tile meets the queries of `window + 127` positions, which start anywhere in a tile
     const long long band = full ? most : std::min(most, ((long long)window + kKeyWeightsKeys - 1) / kKeyWeightsRows + 2);
     pl.key_tiles = (int)(((long long)max_k + kKeyWeightsKeys - 1) / kKeyWeightsKeys);
-    auto chunks = [&](long long tiles) { return (int)std::max(1ll, (tiles + (1ll << pl.chunk_log) - 1) >> pl.chunk_log); };
+    const size_t tile = (size_t)B * Hkv * kKeyWeightsKeys * sizeof(float);
+    auto cut = [&](int chunk_log) {
+        auto chunks = [&](long long tiles) { return (int)std::max(1ll, (tiles + (1ll << chunk_log) - 1) >> chunk_log); };
+        pl.chunk_log = chunk_log;
+        pl.chunks = chunks(band);
+        pl.sink_chunks = full ? 1 : chunks(most);
+        pl.sink_tiles = pl.sink_chunks > pl.chunks ? (int)std::min<long long>(((long long)n_sink + kKeyWeightsKeys - 1) / kKeyWeightsKeys, pl.key_tiles) : 0;
+        pl.off_sink = pl.chunks > 1 ? tile * pl.chunks * pl.key_tiles : 0;
+        pl.bytes = pl.off_sink + tile * pl.sink_chunks * pl.sink_tiles;
+    };
+    cut(kKeyWeightsChunkLog);
     // Calls of few key tiles are cut finer, down to 8 steps a block, until there are two blocks per SM.  Window 2048, us uncut and cut: 1024 tokens,
     // 32 + 8 heads of 128 32.2 and 20.8; 2048 tokens, 28 + 4 heads 94.4 and 44.5; 4096 tokens, window 512 92.8 and 49.5; 500 and 300 tokens 19.9
-    // and 15.6; 8192 tokens, 4 + 2 heads 51.6 and 38.  Until there are four or eight: the same within 4 %.
-    pl.chunk_log = kKeyWeightsChunkLog;
-    while (pl.chunk_log > 0 && (G / pl.heads_per_step) << pl.chunk_log >= 16 && (long long)B * Hkv * pl.key_tiles * chunks(band) < 2ll * sms) --pl.chunk_log;
-    pl.chunks = chunks(band);
-    pl.sink_chunks = full ? 1 : chunks(most);
-    pl.sink_tiles = pl.sink_chunks > pl.chunks ? (int)std::min<long long>(((long long)n_sink + kKeyWeightsKeys - 1) / kKeyWeightsKeys, pl.key_tiles) : 0;
-    const size_t tile = (size_t)B * Hkv * kKeyWeightsKeys * sizeof(float);
-    pl.off_sink = pl.chunks > 1 ? tile * pl.chunks * pl.key_tiles : 0;
-    pl.bytes = std::max(pl.off_sink + tile * pl.sink_chunks * pl.sink_tiles, (size_t)256);
+    // and 15.6; 8192 tokens, 4 + 2 heads 51.6 and 38.  Until there are four or eight: the same within 4 %.  What that takes of the
+    // workspace stays within a bound of its own, which every call is asked for: a workspace for longer sequences does for shorter ones.
+    const size_t fine = 4 * (size_t)sms * kKeyWeightsKeys * sizeof(float);
+    while (pl.chunk_log > 0 && (G / pl.heads_per_step) << pl.chunk_log >= 16 && (long long)B * Hkv * pl.key_tiles * pl.chunks < 2ll * sms) {
+        const KeyWeightsPlan before = pl;
+        cut(pl.chunk_log - 1);
+        if (pl.bytes > fine) {
+            pl = before;
+            break;
+        }
+    }
+    pl.bytes = std::max(pl.bytes, fine);
     return pl;
 }
 

@@ -143,11 +143,19 @@ def test_binding_refuses_shapes_and_kinds(lib):
 
 
 def test_key_weights_workspace_grows_with_what_is_cut(lib):
-    """Chunks of 32 query tiles of 64: nothing is cut up to 2048 queries; under a window the sinks' tiles alone are."""
+    """Chunks of 16 query tiles of 128; below, a bound for what small calls cut finer (4 x 128 sums per SM), whatever the call.  A workspace
+    for longer sequences, more of them or more queries does for less."""
     size = swaa.key_weights_workspace_size
-    assert size(3, 2048, 9000, 8, 2, 1, 0, True) == 256
-    assert size(3, 2049, 9000, 8, 2, 1, 0, True) == 2 * 3 * 2 * 71 * 128 * 4
-    assert size(3, 9000, 9000, 8, 2, 1000, 0, False) == 256
-    assert size(3, 9000, 9000, 8, 2, 1000, 4, False) == 5 * 3 * 2 * 128 * 4
-    assert size(3, 9000, 9000, 8, 2, 1000, 4, False, last=64) == 256
+    least = size(3, 9000, 9000, 8, 2, 1000, 4, False, last=64)
+    assert least % (4 * 128 * 4) == 0 and least == size(1, 1, 1, 1, 1, 1, 0, True)
+    assert size(3, 2049, 90000, 8, 2, 1, 0, True) == 2 * 3 * 2 * 704 * 128 * 4
+    assert size(3, 9000, 9000, 8, 2, 1000, 0, False) == least
+    assert size(300, 9000, 9000, 8, 2, 1000, 4, False) == 5 * 300 * 2 * 128 * 4
     assert size(0, 9000, 9000, 8, 2, 1000, 4, False) == 256
+    for full, window, n_sink in ((True, 1, 0), (False, 300, 4), (False, 2048, 700)):
+        for B in (1, 2, 5, 40):
+            last = 0
+            for n in (1, 70, 128, 500, 1024, 2048, 2100, 4096, 9000, 20000, 70000):
+                now = size(B, n, n, 28, 4, window, n_sink, full)
+                assert now >= last and size(B, min(n, 64), n, 28, 4, window, n_sink, full) <= now and size(max(B // 2, 1), n, n, 28, 4, window, n_sink, full) <= now
+                last = now
