@@ -20,14 +20,6 @@ static int check_rope(int T, int Hq, int Hkv, int D, int rotary_dim, const float
     return SWAA_OK;
 }
 
-constexpr int kRopeBlocksPerSm = 2;
-
-// Blocks of a launch: a warp per share of a token, as many as the SMs hold at a time; the warps go on through the tokens.
-static unsigned rope_blocks(int T, const RopeSplit& s, int sms) {
-    const long long most = std::max((long long)sms * kRopeBlocksPerSm, ((long long)s.segs + kRopeWarps - 1) / kRopeWarps);
-    return (unsigned)std::min(((long long)T * s.segs + kRopeWarps - 1) / kRopeWarps, most);
-}
-
 template <bool kCache>
 static int launch_rope(const RopeParams& p, int D, bool pairs, int sms, cudaStream_t st) {
     const dim3 grid(rope_blocks(p.T, RopeSplit(p.Hq, p.Hkv, D, kRopeRows, p.v != nullptr), sms));

@@ -23,6 +23,8 @@
 // and gradient: 66 + 114 + 4.  Loads into registers instead of the ring 150; three blocks per SM at 80 registers 147 where two take 131.
 #pragma once
 
+#include <algorithm>
+
 #include "swaa_internal.cuh"
 #include "swaa_ptx.cuh"
 
@@ -30,6 +32,7 @@ namespace swaa {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
+constexpr int kRopeBlocksPerSm = 2;
 constexpr int kRopeRows = 4;     // groups of heads of a warp's share of a token: forward
 constexpr int kRopeBwdRows = 2;  // and gradient, which takes two rows of each head
 constexpr int kRopeShare = kRopeRows * 1024;  // bytes of a share: a group is 4 heads of 128 channels or 8 of 64
@@ -52,6 +55,11 @@ struct RopeSplit {
         segs = seg_q + (groups_kv + rows - 1) / rows;
     }
 };
+// Blocks of a launch: a warp per share of a token, as many as the SMs hold at a time; the warps go on through the tokens.
+inline unsigned rope_blocks(int T, const RopeSplit& s, int sms) {
+    const long long most = std::max((long long)sms * kRopeBlocksPerSm, ((long long)s.segs + kRopeWarps - 1) / kRopeWarps);
+    return (unsigned)std::min(((long long)T * s.segs + kRopeWarps - 1) / kRopeWarps, most);
+}
 // A warp's place among them: share `seg` of the tokens stream, stream + streams, ...  Neighbouring warps have the shares of one token, which
 // are neighbours in memory: 16k tokens of 16 + 4 heads of 64, forward and gradient, 63 us; with streams of their own for every kind of head,
 // as many as its work asks for, the kinds drift apart and it takes 97.
@@ -60,16 +68,20 @@ struct RopeWarp {
     static constexpr int kHeads = 32 / (D / 16);
     int seg, stream, streams, groups;
     bool keys;  // keys and values
-    __device__ __forceinline__ RopeWarp(const RopeSplit& p, unsigned warp, unsigned warps) {
+    __host__ __device__ __forceinline__ RopeWarp(const RopeSplit& p, unsigned warp, unsigned warps) {
         seg = (int)(warp % (unsigned)p.segs);
         stream = (int)(warp / (unsigned)p.segs);
         streams = (int)(warps / (unsigned)p.segs);
         keys = seg >= p.seg_q;
-        groups = keys ? min(kRows, p.groups_kv - (seg - p.seg_q) * kRows) : min(kRows, p.groups_q - seg * kRows);
+        const int left = keys ? p.groups_kv - (seg - p.seg_q) * kRows : p.groups_q - seg * kRows;
+        groups = left < kRows ? left : kRows;
     }
+    // Whether the warp has any of the T tokens.  A grid is whole blocks: the last warps may make up no stream of their own, and in a call of
+    // few tokens a stream may start behind the last one.
+    __host__ __device__ __forceinline__ bool works(int T) const { return stream < streams && stream < T; }
     // group u of the share: whether it holds values, and its first head
-    __device__ __forceinline__ bool value(const RopeSplit& p, int u) const { return keys && p.values && ((seg - p.seg_q) * kRows + u) % 2 != 0; }
-    __device__ __forceinline__ int head(const RopeSplit& p, int u) const {
+    __host__ __device__ __forceinline__ bool value(const RopeSplit& p, int u) const { return keys && p.values && ((seg - p.seg_q) * kRows + u) % 2 != 0; }
+    __host__ __device__ __forceinline__ int head(const RopeSplit& p, int u) const {
         const int g = (keys ? seg - p.seg_q : seg) * kRows + u;
         return (keys && p.values ? g / 2 : g) * kHeads;
     }
@@ -300,7 +312,7 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     const RopeSplit split(p.Hq, p.Hkv, D, kRopeRows, p.v != nullptr);
     const RopeWarp<D, kRopeRows> me(split, blockIdx.x * kRopeWarps + (threadIdx.x >> 5), gridDim.x * kRopeWarps);
     const int stream = me.stream, streams = me.streams;
-    if (stream >= streams) return;
+    if (!me.works(p.T)) return;
     const int heads = me.keys ? p.Hkv : p.Hq;
     const float* w = me.keys ? p.kw : p.qw;
     const L ln(lane, p.inv_freq, p.rot);
@@ -435,12 +447,12 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_backward_kernel(const Ro
             if (norm && !value) ring.copy(i, kRopeShare / 2 + u * 1024, (me.keys ? p.k + t * p.k_stride : p.q + t * p.q_stride) + (long long)h0 * D, n);
         }
     };
-    const int T = me.stream < streams ? p.T : 0;  // warps beyond the streams have no tokens
+    const int T = me.works(p.T) ? p.T : 0;  // a warp without tokens still joins the sums of its block
     int filled = 0;
     for (int t = me.stream; filled < kRopeStages && t < T; t += streams, ++filled)
         if (lane == 0) fill(filled, t);
     bool ok = true;
-    int given = me.stream < T ? p.positions[me.stream] : 0;
+    int given = T > 0 ? p.positions[me.stream] : 0;
     for (int t = me.stream; t < T; t += streams) {
         const int position = given;
         if (t < T - streams) given = p.positions[t + streams];  // of the next token, on its way meanwhile
