@@ -341,13 +341,16 @@ __global__ void __launch_bounds__(kRopeThreads, 2) rope_kernel(const RopeParams 
     bool ok = true;
     RopeSeq seq = {0, -1, 0, false};
     // The next token's position on its way during this one: 16k tokens of 16 + 4 heads of 64, forward and gradient, 63.0 -> 58.3 us; not
-    // for packed tokens of heads of 128 (32k tokens, 32 + 8 heads: 145 us without, 153 with).
-    constexpr bool kAhead = kCache || D == 64;
+    // for heads of 128 (32k tokens, 32 + 8 heads: packed 145 us without, 153 with; appended to a cache 146 and 154; 16 generated tokens and a
+    // step of chunks next to tokens the same either way).
+    constexpr bool kAhead = D == 64;
     int given = kAhead && p.positions != nullptr ? p.positions[stream] : 0;
     for (int t = stream; t < p.T; t += streams) {
         int position = given;
-        if (!kAhead) position = p.positions[t];
-        else if (p.positions != nullptr && t < p.T - streams) given = p.positions[t + streams];
+        if (p.positions != nullptr) {
+            if (!kAhead) position = p.positions[t];
+            else if (t < p.T - streams) given = p.positions[t + streams];
+        }
         long long row = t;
         bool store = true;
         if (kCache) {  // the same for the whole warp
