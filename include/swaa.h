@@ -574,7 +574,7 @@ int swaa_decode_weighted_paged(const void* q, const void* kpages, const void* vp
  *   kept            device, int32 [B, Hkv, budget]: their index in the old cache, ascending.  Entries of weights_out and kept from the new
  *                   length on are left as they are.
  *   seqlens_out     device, int32 [B]: min(seqlens[b], budget); not seqlens itself.
- * B at most 65535.
+ * B at most 65535; the smaller of Lmax (max_blocks * page_size) and weights_rows at most 2^31 - 2^16.
  */
 int swaa_cache_evict(const void* kcache, const void* vcache, const float* weights, const int32_t* seqlens, int B, int Lmax,
                      int weights_rows, int Hkv, int D, int budget, int n_sink, int recent, void* kcache_out, void* vcache_out,

@@ -231,6 +231,8 @@ static int evict_impl(EvictParams p, int D, bool paged, cudaStream_t st) {
     if ((long long)p.n_sink + p.recent > p.budget || p.rows_out < p.budget || p.weights_out_rows < p.budget) return SWAA_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return SWAA_ERR_UNSUPPORTED;
     if (p.B > 65535 || (long long)p.B * p.Hkv > 0x7fffffffLL / kEvictMaxCluster) return SWAA_ERR_UNSUPPORTED;  // grid dimensions
+    const int length = std::min(p.rows, p.weights_rows);
+    if (length > 0x7fff0000) return SWAA_ERR_UNSUPPORTED;  // the selection goes through a row in int steps of up to 16384 entries
     if (p.B == 0) return SWAA_OK;
     if (!p.k || !p.v || !p.weights || !p.seqlens || !p.k_out || !p.v_out || !p.weights_out || !p.kept || !p.seqlens_out) return SWAA_ERR_INVALID_ARG;
     if (paged && (!p.block_table || !p.block_table_out)) return SWAA_ERR_INVALID_ARG;
@@ -247,7 +249,6 @@ static int evict_impl(EvictParams p, int D, bool paged, cudaStream_t st) {
     DeviceInfo info;
     int rc = current_sm100(&info);
     if (rc != SWAA_OK) return rc;
-    const int length = std::min(p.rows, p.weights_rows);
     const int ranks = evict_cluster((long long)heads, length, info.sm_count);
     constexpr int kMostKeys = 48 * 1024;
     p.cap = std::min(((length + ranks - 1) / ranks + 3) / 4 * 4, kMostKeys);
