@@ -566,9 +566,9 @@ int swaa_decode_weighted_paged(const void* q, const void* kpages, const void* vp
  *                   reported as SWAA_ERR_BAD_SEQLENS through the status word; seqlens_out is 0 then and nothing is copied.
  *   budget          >= 1, n_sink + recent <= budget.
  *   kcache_out, vcache_out  device, bf16 [B, Lmax_out, Hkv, D], Lmax_out >= budget; or pages of their own size and table.  Rows from
- *                   the new length on are left as they are.  Dense caches must not overlap the old ones (SWAA_ERR_INVALID_ARG); new pages
- *                   may come from the same pool, but must be none that the call reads, nor one another.  A page index outside
- *                   the pool is reported as SWAA_ERR_BAD_SEQLENS and the entries that need it are not copied.
+ *                   the new length on are left as they are.  Dense caches must not overlap the old ones nor each other (SWAA_ERR_INVALID_ARG);
+ *                   new pages may come from the same pool, but must be none that the call reads, nor one another.  A page index
+ *                   outside the pool is reported as SWAA_ERR_BAD_SEQLENS and the entries that need it are not copied.
  *   weights_out     device, float32 [B, Hkv, weights_out_rows], weights_out_rows >= budget: weights of the entries that stay; not overlapping
  *                   weights.
  *   kept            device, int32 [B, Hkv, budget]: their index in the old cache, ascending.  Entries of weights_out and kept from the new

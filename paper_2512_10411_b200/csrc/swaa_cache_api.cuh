@@ -241,7 +241,8 @@ static int evict_impl(EvictParams p, int D, bool paged, cudaStream_t st) {
         !aligned4(p.kept) || !aligned4(p.seqlens_out))
         return SWAA_ERR_INVALID_ARG;
     const size_t heads = (size_t)p.B * p.Hkv, in = heads * p.rows * D * 2, out = heads * p.rows_out * D * 2;
-    if (!paged && (overlap(p.k, in, p.k_out, out) || overlap(p.v, in, p.v_out, out) || overlap(p.k, in, p.v_out, out) || overlap(p.v, in, p.k_out, out)))
+    if (!paged && (overlap(p.k, in, p.k_out, out) || overlap(p.v, in, p.v_out, out) || overlap(p.k, in, p.v_out, out) || overlap(p.v, in, p.k_out, out) ||
+                   overlap(p.k_out, out, p.v_out, out)))
         return SWAA_ERR_INVALID_ARG;
     if (overlap(p.weights, heads * p.weights_rows * 4, p.weights_out, heads * p.weights_out_rows * 4) ||
         overlap(p.seqlens, (size_t)p.B * 4, p.seqlens_out, (size_t)p.B * 4))
