@@ -9,8 +9,9 @@
 // keep y.  Gradient, with g = the rotation by the negative angle of dz:
 //     dw = sum over tokens and heads of g u,     dx = (w g - u mean(w g u)) / sqrt(mean(x^2) + eps)
 //
-// Angles are formed in double: position * frequency / 2 pi keeps its fraction to 2^-24 for every 32-bit position (frequencies up to
-// 1), and sincospif takes the fraction; there is no table whose length bounds the positions.  All sums and products are
+// Angles are formed in double: position * frequency / 2 pi keeps its fraction to 2^-24 for positions up to 2^30 and to 2^-23 for every other
+// 32-bit one (frequencies up to 1), and sincospif takes the fraction; there is no table whose length bounds the positions.  For |position| up
+// to 2^k the rounded product adds 2^(k - 54) / 2 pi, 1 / 2 pi as a double 2^(k - 56), its product 2^(k - 56) and the fraction in fp32 2^-26.  All sums and products are
 // fp32, rounded to bf16 once, at the store.
 //
 // What bounds it: memory, every channel read and written once (2 * 2 bytes a channel; the gradient 3 * 2).  A head is D / 16 lanes,
