@@ -507,7 +507,8 @@ int swaa_cache_append_paged(const void* q, const void* k, const void* v, long lo
  *   weights_out     device, float32 [B, Hkv, weights_rows]; entries from len_k on are left as they are.
  *   last            > 0: only the last `last` queries of every sequence count (what the end of a prompt looks at); 0: all.
  *   workspace       at least swaa_key_weights_workspace_size(...) bytes (paged: max_seqlen_k = the smaller of max_blocks * page_size and
- *                   weights_rows), 256-byte aligned, uninitialised: sums of blocks that share the queries of a key.
+ *                   weights_rows), 256-byte aligned, uninitialised: sums of blocks that share the queries of a key, 32 KB per SM at most
+ *                   whatever the lengths.  A workspace for longer sequences, more of them or more queries does for less.
  * A sequence with len_q > len_k, longer than the stated bounds or than weights_rows is reported as SWAA_ERR_BAD_SEQLENS through the
  * status word and gathers nothing; a page index outside [0, num_pages) likewise, for its keys (pages whose keys no query of the call
  * sees are not looked up).  Sums are taken in a fixed order.  Other

@@ -421,6 +421,13 @@ static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int G, int H
         pl.bytes = pl.off_sink + tile * pl.sink_chunks * pl.sink_tiles;
     };
     cut(kKeyWeightsChunkLog);
+    // Under full attention (and for many sinks) chunks of one length would take a workspace quadratic in the prompt's: they get longer instead, so
+    // that their sums stay within kKeyWeightsPartTiles key tiles per SM, which are blocks enough.  One prompt, 32 + 8 heads of 128, ms and
+    // workspace of 16 query tiles a chunk and of this: 32k tokens 6.0 (17 MB) and 5.2 (4.8 MB), 128k 121 (268 MB) and 87 (4.8 MB); with 256 key
+    // tiles per SM 6.0 and 112.  16 prompts of 32k, window 2048: 14 to 16 either way.
+    const size_t bound = kKeyWeightsPartTiles * (size_t)sms * kKeyWeightsKeys * sizeof(float);
+    const size_t wanted = std::min(pl.bytes, bound);
+    while (pl.bytes > bound) cut(pl.chunk_log + 1);
     // Calls of few key tiles are cut finer, down to 8 steps a block, until there are two blocks per SM.  Window 2048, us uncut and cut: 1024 tokens,
     // 32 + 8 heads of 128 32.2 and 20.8; 2048 tokens, 28 + 4 heads 94.4 and 44.5; 4096 tokens, window 512 92.8 and 49.5; 500 and 300 tokens 19.9
     // and 15.6; 8192 tokens, 4 + 2 heads 51.6 and 38.  Until there are four or eight: the same within 4 %.  What that takes of the
@@ -434,7 +441,7 @@ static KeyWeightsPlan key_weights_plan(int B, int max_q, int max_k, int G, int H
             break;
         }
     }
-    pl.bytes = std::max(pl.bytes, fine);
+    pl.bytes = std::max(wanted, fine);  // at least what the chunks take, and no less than a smaller call asks for
     return pl;
 }
 

@@ -101,6 +101,8 @@ constexpr int kKeyWeightsKeys = 128;
 constexpr int kKeyWeightsRows = 128;   // columns of a step: queries, or queries of two heads in turn
 constexpr int kKeyWeightsChunkLog = 4;  // log2 of the query tiles of a block, less in small calls
 constexpr int kKeyWeightsThreads = 320;  // two groups of four warps, producer, issuer
+constexpr int kKeyWeightsSumSteps = 512;  // steps of a key tile, a power of two, after which the two groups start new sums
+constexpr int kKeyWeightsPartTiles = 64;  // key tiles per SM, each chunk counted, whose sums the chunks of a call may take
 constexpr int kKeyWeightsRunSteps = 16;  // steps below which a block takes more key tiles
 constexpr int kKeyWeightsLse = 4;      // steps whose log-sum-exps are in shared memory
 
@@ -158,7 +160,8 @@ struct KeyWeightsSmem {
     static constexpr int kOffRing = kTileBytes;       // K first
     static constexpr int kOffLse = kOffRing + kStages * kTileBytes;
     static constexpr int kOffSum = kOffLse + kKeyWeightsLse * kKeyWeightsRows * 4;
-    static constexpr int kOffBar = kOffSum + 2 * kKeyWeightsKeys * 4;
+    static constexpr int kOffFar = kOffSum + 2 * kKeyWeightsKeys * 4;
+    static constexpr int kOffBar = kOffFar + 2 * kKeyWeightsKeys * 4;
     static constexpr int kNumBars = 2 + 2 * kStages + 2 * kKeyWeightsLse + 4 + 1;
     static constexpr int kOffMisc = kOffBar + kNumBars * 8;
     static constexpr int kBytes = kOffMisc + 16;
@@ -194,6 +197,7 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     }
     float* s_lse = reinterpret_cast<float*>(smem_raw + L::kOffLse);
     float* s_sum = reinterpret_cast<float*>(smem_raw + L::kOffSum);
+    float* far = reinterpret_cast<float*>(smem_raw + L::kOffFar);  // a word of each thread that sums (a register would spill)
     const uint32_t sK = smem_base, sRing = smem_base + L::kOffRing, bars = smem_base + L::kOffBar;
     auto bar = [&](int i) -> uint32_t { return bars + 8u * (uint32_t)i; };
     constexpr int BAR_KF = 0, BAR_KE = 1, BAR_QF = 2, BAR_QE = BAR_QF + NQ, BAR_LF = BAR_QE + NQ, BAR_LE = BAR_LF + NL, BAR_SF = BAR_LE + NL;
@@ -392,8 +396,9 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             const int j0 = t * BK, jw = j0 + 32 * quad, j = j0 + kl, n_steps = x.nm * head_steps;
             const int vis_hi = (full || j < p.n_sink) ? s.len_k : (int)min((long long)s.len_k, (long long)j + p.window);
             float total = 0.f;
-            int m = (base ^ grp) & 1;  // first step of this group, then every other one
-            for (int i = m; i < n_steps && ok; i += 2) {
+            const int first = (base ^ grp) & 1;  // step of this group, then every other one
+            int m = first;
+            for (int i = first; i < n_steps && ok; i += 2) {
                 const int n = base + i, sl = n % NL;
                 while (m >= x.nm) m -= x.nm;
                 const int i0 = s.pos0 + (x.m_lo + m) * BR;  // position of the first query
@@ -475,11 +480,16 @@ key_weights_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 unpack_f32x2(sum[0], a, c);
                 unpack_f32x2(sum[1], d, e);
                 total += (a + c) + (d + e);  // a step's terms at a time, so that long sums keep their bits
+                if ((i & (kKeyWeightsSumSteps - 1)) >= kKeyWeightsSumSteps - 2) {  // half of that is the group's: a sum of sums in long chunks
+                    far[threadIdx.x] = (i < kKeyWeightsSumSteps ? 0.f : far[threadIdx.x]) + total;
+                    total = 0.f;
+                }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(BAR_LE + sl));
                 __syncwarp();
             }
             base += n_steps;
+            if (((kKeyWeightsSumSteps - 2) | first) < n_steps) total += far[threadIdx.x];
             // The two warps that hold the same keys meet here, whatever their waits gave.  (The first group reads its buffer before it
             // gets to the next meeting, the second writes it again after that one.)
             float* meet = s_sum + (t & 1) * BK;
