@@ -475,7 +475,7 @@ int swaa_qk_norm_rope_backward(const void* q, const void* k, long long q_stride,
  *                   may share a row.
  *   q_out           device, bf16, dense [Tq, Hq, D].
  * Tokens behind cu_seqlens_q[B] are padding: their rows of q_out are left as they are.  A sequence with more new tokens
- * than entries, or more entries than the cache holds, is reported as SWAA_ERR_BAD_SEQLENS through the status word and nothing of
+ * than entries, or new tokens and more entries than the cache holds, is reported as SWAA_ERR_BAD_SEQLENS through the status word and nothing of
  * it is written; a page index outside [0, num_pages) likewise, and the keys and values that would go there are not written.
  * Other arguments as for swaa_qk_norm_rope.
  */
@@ -539,7 +539,9 @@ int swaa_key_weights_paged(const void* q, const void* kpages, const float* lse, 
  *                   entries than weights_rows is reported as SWAA_ERR_BAD_SEQLENS through the status word and gathers nothing.
  *   workspace       at least swaa_decode_weighted_workspace_size(...) bytes (paged: Lmax = max_blocks * page_size), 256-byte aligned,
  *                   uninitialised: the scratch of swaa_decode and 4 bytes per visible entry and query head.
- * B, Hkv at most 65535.  Other arguments and status codes as for swaa_decode, swaa_decode_paged.
+ * B, Hkv at most 65535, Hq / Hkv at most 4096, Lmax (max_blocks * page_size) at most 2^31 - 256.  Probabilities are rounded to bf16 for the
+ * product with V, as in swaa_decode; the weights come from fp32 scores.  Other arguments and status codes as for swaa_decode,
+ * swaa_decode_paged.
  */
 size_t swaa_decode_weighted_workspace_size(int B, int Hq, int Hkv, int D, int Lmax, int window, int n_sink, int is_full);
 int swaa_decode_weighted(const void* q, const void* kcache, const void* vcache, void* out, const float* weights_in,

@@ -516,7 +516,8 @@ decode_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ 
                             oacc[nh][qb][3] *= alpha[1];
                         }
                     }
-                    // P^T as the B fragment: (keys 2c, 2c+1 | 2c+8, 2c+9 ; head g)
+                    // P^T as the B fragment: (keys 2c, 2c+1 | 2c+8, 2c+9 ; head g).  The tensor cores take P in V's type: half a step of bf16,
+                    // 2^-8 of a term at most, in the product with V alone (the row's sum and the gathered weights keep fp32)
                     pb[nh][0] = movmatrix_trans(pack_bf16x2(sacc[nh][0], sacc[nh][1]));
                     pb[nh][1] = movmatrix_trans(pack_bf16x2(sacc[nh][2], sacc[nh][3]));
                 }

@@ -12,10 +12,10 @@
 // One block owns 128 keys of one (sequence, kv head) and walks the 128-query tiles that see them, for every head of the group:
 //     S^T = K Q^T [128 keys x 128 queries], tcgen05.mma, accumulators in tensor memory
 // so that a key is a tensor-memory lane and the sum over queries stays in its thread.  Two groups of four warps take the steps in
-// turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than 16 query tiles (fewer in small calls) is cut into
-// chunks for blocks of their own (every tile under full attention, the sinks under a window); the chunks' sums are added in order by
-// a second kernel, so results do not depend on scheduling.  Where few queries count (the last ones of a prompt) a step takes 64 queries
-// of two heads, and a block several tiles of keys one after another.
+// turn; the log-sum-exps of a step's columns come by cp.async.  A tile seen by more than 16 query tiles (fewer in small calls, more in
+// long ones, so that the sums of all chunks take 32 KB per SM at most) is cut into chunks for blocks of their own (every tile under full
+// attention, the sinks under a window); the chunks' sums are added in order by a second kernel, so results do not depend on scheduling.  Where few queries count (the last ones of a prompt) a step takes 64 queries
+// of two heads, in groups of an even number of them, and a block several tiles of keys one after another.
 //
 // What bounds it: shared memory and the exponentials, one per visible pair.  A step of 128 x 128 moves through shared memory the operands of its
 // products (512 cycles at D = 128), its queries (256) and four readings of the log-sum-exps (128), and takes 1024 cycles of
